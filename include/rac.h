@@ -425,6 +425,78 @@ size_t rac_recon_error_workspace_bytes(void);
 int rac_recon_error(const void *X, const void *X_hat, int64_t T, int32_t d, double *out, void *workspace,
                     size_t workspace_bytes, void *stream);
 
+/* ---------------------------------------------------------------------------------------------
+ * Microscaled 4-bit floating point: direct records (no reference) and products of them.
+ *
+ * The paper sends a state that has no reference yet (the first decode step, Sec. IV-B before Eq. 5) as it stands, and its own
+ * quantiser is an integer one against a reference.  These calls are this library's direct form beside it: a record
+ * holds a row in a form that the tensor cores multiply as it stands, so the partition behind the boundary can take its
+ * first product from what came over the link.  Rows are states or rows of a weight matrix: both operands of a product
+ * have the same records.
+ *
+ * Record of one row of d values (little endian), records back to back:
+ *     codes   d/2 B        e2m1 code of channel c in bits 4*(c%2) .. +3 of byte c/2: sign, two bits of exponent, one of
+ *                          mantissa; the magnitudes are 0, 0.5, 1, 1.5, 2, 3, 4, 6
+ *     scale   d/block B    one byte per block of consecutive channels (below)
+ *     exp     1 B          block 16 only: the row's exponent r, int8
+ *     zero padding to a multiple of 32 bytes (whole memory sectors, so that neighbouring rows share none)
+ * A value is code * s.  With amax the largest magnitude of the block (and, block 16, of the row), and nothing clipping
+ * in either form (scales round up, as Eq. 8b does):
+ *     block 32   s = 2^k, k the smallest integer >= -127 with 6 * 2^k >= amax; byte = k + 127 (e8m0)
+ *     block 16   r = the smallest integer >= -100 with 448 * 6 * 2^r >= amax of the row, 0 for a row of zeros;
+ *                s = v * 2^r, v the smallest e4m3 number with 6 * v * 2^r >= amax; byte = v as e4m3 (bit 7 is zero)
+ *     code       x / s rounded to the nearest e2m1 magnitude, to the even code of two that are equally near; the sign of x
+ * A block of zeros has scale byte 0 and codes of magnitude 0.  A block that holds a NaN or an infinity has the scale byte
+ * of NaN (127 with block 16, 255 with block 32) and codes 0, and does not count towards r: it decodes to NaN, makes the
+ * row of a product NaN, and leaves every other block alone.  A row depends on nothing but itself: any range of rows is a contiguous byte
+ * range, and rows may be coded in any split into calls.
+ *
+ *   d        row length: a multiple of 32, 32 .. 32768
+ *   block    16 or 32
+ *   x_type   type of X and X_hat: RAC_MX_BF16 or RAC_MX_FP16
+ *   y_type   type of Y: RAC_MX_BF16, RAC_MX_FP16 or RAC_MX_FP32
+ *   flags    must be 0 */
+#define RAC_MX_BF16 0
+#define RAC_MX_FP16 1
+#define RAC_MX_FP32 2
+typedef struct {
+    int32_t d, block, x_type, y_type, flags;
+} rac_mx_cfg;
+
+/* Record stride in bytes (0 for an invalid configuration) and bytes of T records. */
+size_t rac_mx_record_bytes(const rac_mx_cfg *cfg);
+size_t rac_mx_payload_bytes(const rac_mx_cfg *cfg, int64_t T);
+
+/* X [T,d] to records; with X_hat (may be NULL) also what rac_mx_decode makes of them, bit for bit, in the same pass.
+ *   payload  >= T*record bytes, 16-byte aligned; payload_cap is its capacity.  Every byte of the T records is written.
+ *   X_hat    [T,d]; it may be the very buffer X, and must not overlap X in another way, nor the payload
+ * Sets RAC_STATUS_NONFINITE when a block held a NaN or an infinity. */
+int rac_mx_encode(const rac_mx_cfg *cfg, const void *X, int64_t T, void *payload, size_t payload_cap, void *X_hat,
+                  uint32_t *dev_status, void *stream);
+
+/* Records to X_hat [T,d]: code * s, rounded once to x_type; what lies beyond its largest finite value becomes that.
+ * (A code times a scale has six significant bits: with bf16 nothing is rounded.)  Bit 7 of a block-16 scale is not
+ * read, a row exponent above 117 is taken for 117.  X_hat must not overlap the payload. */
+int rac_mx_decode(const rac_mx_cfg *cfg, const void *payload, int64_t T, void *X_hat, uint32_t *dev_status, void *stream);
+
+/* Y[M,N] = A * B^T for records A of M rows and records B of N rows (a weight matrix [N,d], one record per output
+ * feature): sums in binary32, rounded once to y_type (beyond its largest finite value: an infinity).
+ * The products of two codes and of two scales are exact; the order of the sums depends on the sizes and is the same on every run.
+ *   Y        [M,N], 16-byte aligned, N any number; must not overlap A or B
+ * M and N below 2^31.  M == 0 or N == 0: nothing to do. */
+int rac_mx_product(const rac_mx_cfg *cfg, const void *A, int64_t M, const void *B, int64_t N, void *Y,
+                   uint32_t *dev_status, void *stream);
+
+/* The same with one weight matrix per segment of rows (rows sorted by expert, by adapter):
+ *     Y[t,n] = sum_k A[t,k] * B[s,n,k]     for seg_off[s] <= t < seg_off[s+1]
+ *   seg_off  device int32[n_seg+1], ascending; equal neighbours = an empty segment.  The lengths stay on the device.
+ *   B        records of n_seg*N rows: matrix s is the rows s*N .. s*N+N
+ * Rows of Y that no segment holds (before seg_off[0], from seg_off[n_seg] on) are left as they are.  Offsets outside
+ * [0, M] are clipped into it and a segment whose end lies before its start is empty; where segments overlap, the
+ * overlapping rows hold the product of one of them.  n_seg at most 65535, n_seg*N below 2^31. */
+int rac_mx_product_segments(const rac_mx_cfg *cfg, const void *A, int64_t M, const int32_t *seg_off, int64_t n_seg,
+                            const void *B, int64_t N, void *Y, uint32_t *dev_status, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

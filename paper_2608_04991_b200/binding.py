@@ -41,6 +41,8 @@ EXPORTS = [
     "rac_calibrate_workspace_bytes", "rac_calibrate_steps", "rac_calibrate_steps_shared",
     "rac_recon_error_workspace_bytes", "rac_recon_error",
     "rac_selftest_bounded_wait",
+    "rac_mx_record_bytes", "rac_mx_payload_bytes", "rac_mx_encode", "rac_mx_decode", "rac_mx_product",
+    "rac_mx_product_segments",
 ]
 
 
@@ -70,6 +72,21 @@ class IndexCfg(C.Structure):
 
     def __init__(self, capacity: int, min_ngram: int = 4, max_hits: int = 8):
         super().__init__(capacity, min_ngram, max_hits)
+
+
+class MxCfg(C.Structure):
+    """Mirror of ``rac_mx_cfg``.  ``x_type`` (of X and X_hat) and ``y_type`` (of Y) are torch types."""
+    _fields_ = [(n, C.c_int32) for n in ("d", "block", "x_type", "y_type", "flags")]
+    _types = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
+
+    def __init__(self, d: int, block: int = 16, x_type: torch.dtype = torch.bfloat16, y_type: torch.dtype = torch.bfloat16):
+        if x_type not in self._types or y_type not in self._types:
+            raise TypeError("x_type, y_type: expected torch.bfloat16, torch.float16 or torch.float32")
+        super().__init__(d, block, self._types[x_type], self._types[y_type], 0)
+
+    def __repr__(self):
+        names = {v: str(k).replace("torch.", "") for k, v in self._types.items()}
+        return f"MxCfg(d={self.d}, block={self.block}, x_type={names.get(self.x_type)}, y_type={names.get(self.y_type)})"
 
 
 _lib: Optional[C.CDLL] = None
@@ -197,8 +214,21 @@ def load():
     l.rac_calibrate_steps.argtypes = [cfgp, vp, i64, vp, i64, vp, vp, vp, C.c_float, vp, vp, vp, sz, vp, vp]
     l.rac_calibrate_steps_shared.restype = C.c_int
     l.rac_calibrate_steps_shared.argtypes = [cfgp, vp, i64, vp, i64, vp, vp, vp, vp, vp, C.c_float, vp, vp, vp, sz, vp, vp]
+    mcfgp = C.POINTER(MxCfg)
+    l.rac_mx_record_bytes.restype = sz
+    l.rac_mx_record_bytes.argtypes = [mcfgp]
+    l.rac_mx_payload_bytes.restype = sz
+    l.rac_mx_payload_bytes.argtypes = [mcfgp, i64]
+    l.rac_mx_encode.restype = C.c_int
+    l.rac_mx_encode.argtypes = [mcfgp, vp, i64, vp, sz, vp, vp, vp]
+    l.rac_mx_decode.restype = C.c_int
+    l.rac_mx_decode.argtypes = [mcfgp, vp, i64, vp, vp, vp]
+    l.rac_mx_product.restype = C.c_int
+    l.rac_mx_product.argtypes = [mcfgp, vp, i64, vp, i64, vp, vp, vp]
+    l.rac_mx_product_segments.restype = C.c_int
+    l.rac_mx_product_segments.argtypes = [mcfgp, vp, i64, vp, i64, vp, i64, vp, vp, vp]
     from . import _native as native
-    native.setup(_check, _stream_address, CodecCfg, IndexCfg)
+    native.setup(_check, _stream_address, CodecCfg, IndexCfg, MxCfg)
     _native = native
     _lib = l
     return l
@@ -405,3 +435,31 @@ def rac_calibrate_steps_shared(cfg, X, T, ref_base, ref_rows, ref_row, ref_gain,
                                clip_sigmas, step, inv_step, workspace, workspace_bytes, dev_status, stream=None) -> None:
     _calls().rac_calibrate_steps_shared(cfg, X, T, ref_base, ref_rows, ref_row, ref_gain, ref_bias, coef_seg, seg_of,
                                         clip_sigmas, step, inv_step, workspace, workspace_bytes, dev_status, stream)
+
+
+# ----------------------------------------------------------------------------- microscaled 4-bit records
+def rac_mx_record_bytes(cfg: MxCfg) -> int:
+    return int(load().rac_mx_record_bytes(C.byref(cfg)))
+
+
+def rac_mx_payload_bytes(cfg: MxCfg, T: int) -> int:
+    return int(load().rac_mx_payload_bytes(C.byref(cfg), int(T)))
+
+
+def rac_mx_encode(cfg, X, T, payload, payload_cap, X_hat, dev_status, stream=None) -> None:
+    """Rows to records; ``X_hat`` (or None) receives the values the records stand for in the same pass."""
+    _calls().rac_mx_encode(cfg, X, T, payload, payload_cap, X_hat, dev_status, stream)
+
+
+def rac_mx_decode(cfg, payload, T, X_hat, dev_status, stream=None) -> None:
+    _calls().rac_mx_decode(cfg, payload, T, X_hat, dev_status, stream)
+
+
+def rac_mx_product(cfg, A, M, B, N, Y, dev_status, stream=None) -> None:
+    """Y[M,N] = A B^T for records A of M rows and B of N rows."""
+    _calls().rac_mx_product(cfg, A, M, B, N, Y, dev_status, stream)
+
+
+def rac_mx_product_segments(cfg, A, M, seg_off, n_seg, B, N, Y, dev_status, stream=None) -> None:
+    """The product with one weight matrix per segment of rows; ``seg_off`` is int32[n_seg + 1] on the device."""
+    _calls().rac_mx_product_segments(cfg, A, M, seg_off, n_seg, B, N, Y, dev_status, stream)

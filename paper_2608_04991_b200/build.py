@@ -12,8 +12,9 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "librac.so")
 NATIVE = os.path.join(HERE, "_native" + sysconfig.get_config_var("EXT_SUFFIX"))
 NATIVE_SOURCES = ["rac_py.cpp", os.path.join("..", "..", "include", "rac.h")]
-SOURCES = ["rac_codec.cu", "rac_codec_dyn.cu", "rac_calib.cu", "rac_match.cu"]
-HEADERS = ["rac_common.cuh", "rac_codec_dev.cuh", os.path.join("..", "..", "include", "rac.h")]
+SOURCES = ["rac_codec.cu", "rac_codec_dyn.cu", "rac_calib.cu", "rac_match.cu", "rac_mx.cu",
+           "rac_mx_product.cu"]
+HEADERS = ["rac_common.cuh", "rac_codec_dev.cuh", "rac_mx.cuh", os.path.join("..", "..", "include", "rac.h")]
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
     "-Xcompiler", "-fPIC", "-shared", "--threads", "0", "-Xptxas", "-v",

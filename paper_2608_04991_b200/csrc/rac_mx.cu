@@ -1,0 +1,316 @@
+// Microscaled 4-bit records for sm_100a: encode (values to e2m1 codes with block scales, optionally the values they stand
+// for in the same pass) and decode.  The products of such records are in rac_mx_product.cu.
+//
+// Both kernels stream: a thread has 16 consecutive channels (one block of 16, half a block of 32), a CTA has as many whole
+// rows as fit its threads.  What bounds them is memory: 2 bytes in and 0.57 (+ 2 with x_hat) out per value.
+#include "rac_mx.cuh"
+
+namespace rac {
+
+struct MxParams {
+    const uint8_t *X;        // [T,d], two bytes a value
+    uint8_t *payload;
+    uint8_t *X_hat;
+    uint32_t *status;
+    int64_t T;
+    int d, rec, scale_off, nblk;
+    int tpr;                 // threads per row: d/16
+    int rows;                // rows per CTA
+};
+
+// The eight values of a word of codes times s, in the type of X: four words.
+//
+// A code has two significant bits and a scale four, so the product is exact in bf16 and, where nothing underflows, in
+// binary16.  `fast` (0 or 2^-14 <= s <= 2^13) says that s and every product are normal numbers of both types: then one packed
+// multiplication does two values.  bf16: the bits of the binary16 code, shifted down by three, are the code times 2^-112 as
+// bf16; the factor is made up for in the scale.  Otherwise binary32, rounded once, no further than the largest finite value.
+template <bool HALF>
+__device__ __forceinline__ uint4 mx_values(uint32_t w, float s, bool fast) {
+    uint32_t h[4], o[4];
+    mx_e2m1_to_half(w, h);
+    if (fast) {
+        if constexpr (HALF) {
+            const __half2 f = __float2half2_rn(s);
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                const __half2 v = __hmul2(*reinterpret_cast<__half2 *>(&h[i]), f);
+                o[i] = *reinterpret_cast<const uint32_t *>(&v);
+            }
+        } else {
+            const __nv_bfloat162 f = __float2bfloat162_rn(s * 5.192296858534828e33f);   // 2^112
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                uint32_t b = (h[i] & 0x80008000u) | ((h[i] >> 3) & 0x0fff0fffu);
+                const __nv_bfloat162 v = __hmul2(*reinterpret_cast<__nv_bfloat162 *>(&b), f);
+                o[i] = *reinterpret_cast<const uint32_t *>(&v);
+            }
+        }
+    } else {
+        const float top = HALF ? 65504.0f : __uint_as_float(0x7f7f0000u);
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            float2 v = __half22float2(*reinterpret_cast<__half2 *>(&h[i]));
+            v.x *= s;
+            v.y *= s;
+            v.x = fabsf(v.x) > top ? copysignf(top, v.x) : v.x;   // a NaN stays one
+            v.y = fabsf(v.y) > top ? copysignf(top, v.y) : v.y;
+            if constexpr (HALF) {
+                const __half2 r = __floats2half2_rn(v.x, v.y);
+                o[i] = *reinterpret_cast<const uint32_t *>(&r);
+            } else {
+                o[i] = f2_to_bf16x2(v.x, v.y);
+            }
+        }
+    }
+    return make_uint4(o[0], o[1], o[2], o[3]);
+}
+__device__ __forceinline__ bool mx_fast_scale(float s) { return s == 0.0f || (s >= 6.103515625e-05f && s <= 8192.0f); }
+
+// Codes, scales and exponent of a row, and with XHAT the values they stand for.
+//
+// The quotient x / s decides integers, so it must not be off where it lands on the middle between two codes.  The reciprocal
+// of s is off by half an ulp; x has at most 11 significant bits and a middle times s at most 7, so a quotient that is not a
+// middle is at least 2^-13 away from it.  One fused multiply-add onto 192 = 1.5 * 2^7 rounds the quotient to a multiple of
+// 2^-16, which puts a middle where it belongs and moves no other value across one; then the conversion rounds as specified.
+template <bool HALF, int BLOCK, bool XHAT, int CHUNKS>
+__global__ void mx_encode_kernel(const MxParams p) {
+    extern __shared__ uint32_t row_max[];          // BLOCK 16: bits of the largest finite-block magnitude, per row of the CTA
+    constexpr uint32_t kInf = HALF ? 0x7c00u : 0x7f80u;
+    const int tid = threadIdx.x;
+    const int r = tid / p.tpr;                     // row within the CTA (CHUNKS > 1: always 0)
+    const int64_t row = static_cast<int64_t>(blockIdx.x) * p.rows + r;
+    const bool live = r < p.rows && row < p.T;
+    const int c0 = tid - r * p.tpr;
+    if (BLOCK == 16) {
+        if (tid < p.rows) row_max[tid] = 0;
+    }
+    grid_dependency_wait();
+    if (BLOCK == 16) __syncthreads();
+
+    uint4 x[CHUNKS][2];
+    uint32_t amax[CHUNKS];
+    uint32_t bad = 0, most = 0;
+#pragma unroll
+    for (int k = 0; k < CHUNKS; k++) {
+        const int c = c0 + k * blockDim.x;
+        amax[k] = 0;
+        if (live && (CHUNKS == 1 || c < p.tpr)) {
+            const uint4 *src = reinterpret_cast<const uint4 *>(p.X + (row * p.d + 16 * static_cast<int64_t>(c)) * 2);
+            x[k][0] = src[0];
+            x[k][1] = src[1];
+            const uint32_t *w = reinterpret_cast<const uint32_t *>(&x[k][0]);
+            uint32_t m = w[0] & 0x7fff7fffu;
+#pragma unroll
+            for (int i = 1; i < 8; i++) m = __vmaxu2(m, w[i] & 0x7fff7fffu);
+            amax[k] = max(m & 0xffffu, m >> 16);
+        }
+        if (BLOCK == 32) amax[k] = max(amax[k], __shfl_xor_sync(0xffffffffu, amax[k], 1));
+        if (amax[k] >= kInf) {
+            bad |= 1u << k;
+            amax[k] = 0;
+        }
+        most = max(most, amax[k]);
+    }
+    int rexp = 0;
+    if (BLOCK == 16) {
+        const int first = __shfl_sync(0xffffffffu, r, 0);
+        if (__all_sync(0xffffffffu, r == first)) {
+            const uint32_t m = __reduce_max_sync(0xffffffffu, most);
+            if ((tid & 31) == 0 && first < p.rows && m) atomicMax(&row_max[first], m);
+        } else if (live && most) {
+            atomicMax(&row_max[r], most);
+        }
+        __syncthreads();
+        if (r < p.rows) {
+            const uint32_t m16 = row_max[r];
+            const uint32_t f = __float_as_uint(HALF ? half_bits_to_float(m16) : __uint_as_float(m16 << 16));
+            // f = 1.m * 2^(e-127): 2688 = 1.3125 * 2^11
+            if (f) rexp = max(-100, static_cast<int>(f >> 23) - 138 + ((f & 0x7fffffu) > 0x280000u));
+        }
+    }
+    if (!live) return;
+    uint8_t *rec = p.payload + row * p.rec;
+#pragma unroll
+    for (int k = 0; k < CHUNKS; k++) {
+        const int c = c0 + k * blockDim.x;
+        if (CHUNKS > 1 && c >= p.tpr) break;
+        const float a = HALF ? half_bits_to_float(amax[k]) : __uint_as_float(amax[k] << 16);
+        uint32_t byte;
+        float s, inv;
+        if (BLOCK == 32) {
+            const uint32_t f = __float_as_uint(a);
+            const int e = static_cast<int>(f >> 23) - 2 + ((f & 0x7fffffu) > 0x400000u);     // 6 = 1.5 * 2^2
+            byte = f ? max(0, e) : 0;
+            s = f ? mx_e8m0(byte) : 0.0f;
+            inv = __uint_as_float((254u - byte) << 23);
+        } else {
+            const float b = a * mx_pow2(-rexp);                  // exact
+            uint16_t q;                                          // nearest e4m3, then the next one where that is too small
+            asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(q) : "f"(0.0f), "f"(b * (1.0f / 6.0f)));
+            byte = q & 127u;
+            byte += 6.0f * mx_e4m3(byte) < b;
+            const float v = mx_e4m3(byte);
+            s = v * mx_pow2(rexp);
+            inv = __frcp_rn(v > 0.0f ? v : 1.0f) * mx_pow2(-rexp);
+        }
+        const bool none = bad >> k & 1u;
+        if (none) {
+            byte = BLOCK == 32 ? 255u : 127u;
+            s = __uint_as_float(0x7fc00000u);
+        }
+        const uint32_t *w = reinterpret_cast<const uint32_t *>(&x[k][0]);
+        const float2 inv2 = make_float2(inv, inv), snap = make_float2(192.0f, 192.0f);
+        uint32_t codes[2];
+#pragma unroll
+        for (int half = 0; half < 2; half++) {
+            float2 y[4];
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                const uint32_t u = w[half * 4 + i];
+                const float2 v = HALF ? __half22float2(*reinterpret_cast<const __half2 *>(&u)) : bf16x2_to_f2(u);
+                y[i] = sub2(fma2(v, inv2, snap), snap);
+            }
+            codes[half] = mx_e2m1_from_float(y);
+            // what rounds to nothing comes out of the subtraction as +0: the sign is that of x
+            const uint32_t sign = (w[half * 4] >> 12 & 0x8u) | (w[half * 4] >> 24 & 0x80u) | (w[half * 4 + 1] >> 4 & 0x800u) |
+                                  (w[half * 4 + 1] >> 16 & 0x8000u) | (w[half * 4 + 2] << 4 & 0x80000u) |
+                                  (w[half * 4 + 2] >> 8 & 0x800000u) | (w[half * 4 + 3] << 12 & 0x8000000u) |
+                                  (w[half * 4 + 3] & 0x80000000u);
+            codes[half] = (codes[half] & 0x77777777u) | sign;
+            if (none) codes[half] = 0;
+        }
+        *reinterpret_cast<uint2 *>(rec + 8 * c) = make_uint2(codes[0], codes[1]);
+        if (BLOCK == 16) rec[p.scale_off + c] = static_cast<uint8_t>(byte);
+        else if ((c & 1) == 0) rec[p.scale_off + (c >> 1)] = static_cast<uint8_t>(byte);
+        if (XHAT) {
+            uint4 *dst = reinterpret_cast<uint4 *>(p.X_hat + (row * p.d + 16 * static_cast<int64_t>(c)) * 2);
+            const bool fast = mx_fast_scale(s);
+            dst[0] = mx_values<HALF>(codes[0], s, fast);
+            dst[1] = mx_values<HALF>(codes[1], s, fast);
+        }
+    }
+    // behind the scales: the exponent, zeros
+    const int step = CHUNKS > 1 ? static_cast<int>(blockDim.x) : p.tpr;
+    for (int i = p.scale_off + p.nblk + c0; i < p.rec; i += step)
+        rec[i] = BLOCK == 16 && i == p.scale_off + p.nblk ? static_cast<uint8_t>(rexp) : 0;
+    if (bad && p.status) atomicOr(p.status, RAC_STATUS_NONFINITE);
+}
+
+template <bool HALF, int BLOCK>
+__global__ void mx_decode_kernel(const MxParams p) {
+    const int r = threadIdx.x / p.tpr;
+    const int64_t row = static_cast<int64_t>(blockIdx.x) * p.rows + r;
+    grid_dependency_wait();
+    if (r >= p.rows || row >= p.T) return;
+    const uint8_t *rec = p.payload + row * p.rec;
+    for (int c = threadIdx.x - r * p.tpr; c < p.tpr; c += blockDim.x) {
+        const uint2 codes = *reinterpret_cast<const uint2 *>(rec + 8 * c);
+        float s;
+        if (BLOCK == 32) {
+            const uint32_t b = rec[p.scale_off + (c >> 1)];
+            s = b == 255 ? __uint_as_float(0x7fc00000u) : mx_e8m0(b);
+        } else {
+            const int e = mx_row_exp(rec, p.scale_off + p.nblk);
+            s = mx_e4m3(rec[p.scale_off + c]) * mx_pow2(max(e, -126)) * (e < -126 ? mx_pow2(e + 126) : 1.0f);
+        }
+        uint4 *dst = reinterpret_cast<uint4 *>(p.X_hat + (row * p.d + 16 * static_cast<int64_t>(c)) * 2);
+        const bool fast = mx_fast_scale(s);
+        dst[0] = mx_values<HALF>(codes.x, s, fast);
+        dst[1] = mx_values<HALF>(codes.y, s, fast);
+        if (p.tpr <= static_cast<int>(blockDim.x)) break;      // several rows of the CTA: one piece per thread
+    }
+}
+
+static void mx_shape(const MxGeometry &g, int64_t T, MxParams *p, unsigned *grid, unsigned *threads, int most) {
+    p->T = T;
+    p->d = g.d;
+    p->rec = g.rec;
+    p->scale_off = g.scale_off;
+    p->nblk = g.nblk;
+    p->tpr = g.d / 16;
+    p->rows = p->tpr >= 256 ? 1 : 256 / p->tpr;
+    if (p->rows > T) p->rows = static_cast<int>(T);
+    const int t = p->rows * p->tpr;
+    *threads = static_cast<unsigned>(t > most ? most : (t + 31) / 32 * 32);
+    *grid = static_cast<unsigned>((T + p->rows - 1) / p->rows);
+}
+
+template <bool HALF, int BLOCK, bool XHAT>
+static void launch_mx_encode(const MxParams &p, unsigned grid, unsigned threads, cudaStream_t s) {
+    const size_t smem = BLOCK == 16 ? sizeof(uint32_t) * p.rows : 0;
+    if (p.tpr > 1024) launch_after(mx_encode_kernel<HALF, BLOCK, XHAT, 2>, grid, threads, smem, s, p);
+    else launch_after(mx_encode_kernel<HALF, BLOCK, XHAT, 1>, grid, threads, smem, s, p);
+}
+
+}  // namespace rac
+
+using namespace rac;
+
+extern "C" {
+
+size_t rac_mx_record_bytes(const rac_mx_cfg *cfg) {
+    MxGeometry g;
+    return mx_geometry(cfg, &g) == RAC_OK ? static_cast<size_t>(g.rec) : 0;
+}
+
+size_t rac_mx_payload_bytes(const rac_mx_cfg *cfg, int64_t T) {
+    return T < 0 ? 0 : rac_mx_record_bytes(cfg) * static_cast<size_t>(T);
+}
+
+int rac_mx_encode(const rac_mx_cfg *cfg, const void *X, int64_t T, void *payload, size_t payload_cap, void *X_hat,
+                  uint32_t *dev_status, void *stream) {
+    MxGeometry g;
+    const int rc = mx_geometry(cfg, &g);
+    if (rc != RAC_OK) return rc;
+    if (T < 0) return RAC_EINVAL;
+    if (T == 0) return RAC_OK;
+    if (T > INT32_MAX) return RAC_EUNSUPPORTED;
+    if (!X || !payload) return RAC_EINVAL;
+    if (!mx_aligned(X) || !mx_aligned(payload) || !mx_aligned(X_hat)) return RAC_EALIGN;
+    const size_t nx = static_cast<size_t>(T) * g.d * 2, np = static_cast<size_t>(T) * g.rec;
+    if (payload_cap < np) return RAC_ESIZE;
+    if (mx_overlap(X, nx, payload, np)) return RAC_EINVAL;
+    if (X_hat && (mx_overlap(X_hat, nx, payload, np) || (X_hat != X && mx_overlap(X_hat, nx, X, nx)))) return RAC_EINVAL;
+    MxParams p = {};
+    unsigned grid, threads;
+    mx_shape(g, T, &p, &grid, &threads, 1024);
+    p.X = static_cast<const uint8_t *>(X);
+    p.payload = static_cast<uint8_t *>(payload);
+    p.X_hat = static_cast<uint8_t *>(X_hat);
+    p.status = dev_status;
+    auto s = static_cast<cudaStream_t>(stream);
+    const bool half = g.x_type == RAC_MX_FP16;
+    if (g.block == 16) {
+        if (X_hat) half ? launch_mx_encode<true, 16, true>(p, grid, threads, s) : launch_mx_encode<false, 16, true>(p, grid, threads, s);
+        else half ? launch_mx_encode<true, 16, false>(p, grid, threads, s) : launch_mx_encode<false, 16, false>(p, grid, threads, s);
+    } else {
+        if (X_hat) half ? launch_mx_encode<true, 32, true>(p, grid, threads, s) : launch_mx_encode<false, 32, true>(p, grid, threads, s);
+        else half ? launch_mx_encode<true, 32, false>(p, grid, threads, s) : launch_mx_encode<false, 32, false>(p, grid, threads, s);
+    }
+    return cudaGetLastError() == cudaSuccess ? RAC_OK : RAC_ECUDA;
+}
+
+int rac_mx_decode(const rac_mx_cfg *cfg, const void *payload, int64_t T, void *X_hat, uint32_t *dev_status, void *stream) {
+    MxGeometry g;
+    const int rc = mx_geometry(cfg, &g);
+    if (rc != RAC_OK) return rc;
+    if (T < 0) return RAC_EINVAL;
+    if (T == 0) return RAC_OK;
+    if (T > INT32_MAX) return RAC_EUNSUPPORTED;
+    if (!payload || !X_hat) return RAC_EINVAL;
+    if (!mx_aligned(payload) || !mx_aligned(X_hat)) return RAC_EALIGN;
+    if (mx_overlap(X_hat, static_cast<size_t>(T) * g.d * 2, payload, static_cast<size_t>(T) * g.rec)) return RAC_EINVAL;
+    (void)dev_status;      // nothing in a record is out of range; kept for the shape of the calls
+    MxParams p = {};
+    unsigned grid, threads;
+    mx_shape(g, T, &p, &grid, &threads, 1024);
+    p.payload = const_cast<uint8_t *>(static_cast<const uint8_t *>(payload));
+    p.X_hat = static_cast<uint8_t *>(X_hat);
+    auto s = static_cast<cudaStream_t>(stream);
+    const bool half = g.x_type == RAC_MX_FP16;
+    if (g.block == 16) half ? launch_after(mx_decode_kernel<true, 16>, grid, threads, 0, s, p) : launch_after(mx_decode_kernel<false, 16>, grid, threads, 0, s, p);
+    else half ? launch_after(mx_decode_kernel<true, 32>, grid, threads, 0, s, p) : launch_after(mx_decode_kernel<false, 32>, grid, threads, 0, s, p);
+    return cudaGetLastError() == cudaSuccess ? RAC_OK : RAC_ECUDA;
+}
+
+}  // extern "C"

@@ -6,6 +6,7 @@
 // argument is taken from its declaration in rac.h.
 #include <Python.h>
 
+#include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -47,7 +48,8 @@ constexpr int length(const char *s) {
 }
 
 constexpr int kMaxArgs = 24;
-// kinds: c rac_codec_cfg, x rac_index_cfg; tensors or addresses: b bf16, h binary16, f float32, i int32, u bytes, a any type;
+// kinds: c rac_codec_cfg, x rac_index_cfg, m rac_mx_cfg (first, where X and Y occur); tensors or addresses: b bf16, h binary16, f float32, i int32, u bytes, a any type,
+// X and Y the types x_type and y_type of the rac_mx_cfg (and, like every tensor of such a call, on the current device);
 // numbers: l integer, B truth value, d float; s stream (None = the current one, an address, or what ctypes takes for one)
 struct Entry {
     const char *name, *kinds, *args;   // args: names, comma separated (for messages)
@@ -101,10 +103,18 @@ const Entry kEntries[] = {
               "cfg,X,T,ref_base,ref_rows,ref_row,ref_gain,ref_bias,coef_seg,seg_of,clip_sigmas,step,inv_step,workspace,workspace_bytes,dev_status,stream"),
     RAC_ENTRY(rac_recon_error, "bbllaals",
               "X,X_hat,T,d,out,workspace,workspace_bytes,stream"),
+    RAC_ENTRY(rac_mx_encode, "mXlulXis",
+              "cfg,X,T,payload,payload_cap,X_hat,dev_status,stream"),
+    RAC_ENTRY(rac_mx_decode, "mulXis",
+              "cfg,payload,T,X_hat,dev_status,stream"),
+    RAC_ENTRY(rac_mx_product, "mululYis",
+              "cfg,A,M,B,N,Y,dev_status,stream"),
+    RAC_ENTRY(rac_mx_product_segments, "mulilulYis",
+              "cfg,A,M,seg_off,n_seg,B,N,Y,dev_status,stream"),
 };
 
 PyObject *g_check = nullptr;   // binding._check(name, return code): raises for a non-zero code
-PyObject *g_codec_cfg = nullptr, *g_index_cfg = nullptr;   // binding.CodecCfg, binding.IndexCfg: the structs of rac.h
+PyObject *g_codec_cfg = nullptr, *g_index_cfg = nullptr, *g_mx_cfg = nullptr;   // binding.CodecCfg, .IndexCfg, .MxCfg: the structs of rac.h
 PyObject *g_stream = nullptr;  // binding._stream_address(object) -> int, for streams that are neither None nor an address
 
 const char *arg_name(const Entry &e, int k, char *buf, size_t cap) {
@@ -147,9 +157,14 @@ bool as_integer(PyObject *o, long long *out) {
     return !(*out == -1 && PyErr_Occurred());
 }
 
-// one argument; false with a Python error set
-bool marshal(const Entry &e, int k, PyObject *o, Slot *s) {
-    const char kind = e.kinds[k];
+// the letter of a type of rac_mx_cfg (a type that is none is for the library to refuse)
+char mx_kind(int32_t type) { return type == RAC_MX_FP32 ? 'f' : type == RAC_MX_FP16 ? 'h' : 'b'; }
+
+// one argument; false with a Python error set.  `first`: the call's first argument, marshalled before any other
+bool marshal(const Entry &e, int k, PyObject *o, Slot *s, const Slot *first) {
+    char kind = e.kinds[k];
+    if (kind == 'X') kind = mx_kind(static_cast<const rac_mx_cfg *>(first->p)->x_type);
+    else if (kind == 'Y') kind = mx_kind(static_cast<const rac_mx_cfg *>(first->p)->y_type);
     char name[32];
     switch (kind) {
         case 'l':
@@ -179,10 +194,12 @@ bool marshal(const Entry &e, int k, PyObject *o, Slot *s) {
             }
             return as_integer(o, &s->i);
         case 'c':
-        case 'x': {
+        case 'x':
+        case 'm': {
+            PyObject *type = kind == 'c' ? g_codec_cfg : kind == 'x' ? g_index_cfg : g_mx_cfg;
             // the struct type itself (or a subclass): any other buffer of its size is none
-            if (!PyObject_TypeCheck(o, reinterpret_cast<PyTypeObject *>(kind == 'c' ? g_codec_cfg : g_index_cfg))) {
-                PyErr_Format(PyExc_TypeError, "%s: expected %s", arg_name(e, k, name, sizeof name), kind == 'c' ? "a CodecCfg" : "an IndexCfg");
+            if (!PyObject_TypeCheck(o, reinterpret_cast<PyTypeObject *>(type))) {
+                PyErr_Format(PyExc_TypeError, "%s: expected %s", arg_name(e, k, name, sizeof name), kind == 'c' ? "a CodecCfg" : kind == 'x' ? "an IndexCfg" : "an MxCfg");
                 return false;
             }
             Py_buffer v;
@@ -214,6 +231,10 @@ bool marshal(const Entry &e, int k, PyObject *o, Slot *s) {
         PyErr_Format(PyExc_TypeError, "%s: expected %s, got %s", arg_name(e, k, name, sizeof name), kind_name(kind), c10::toString(t.scalar_type()));
         return false;
     }
+    if (e.kinds[0] == 'm' && t.get_device() != c10::cuda::current_device()) {
+        PyErr_Format(PyExc_ValueError, "%s: must be on the current CUDA device", arg_name(e, k, name, sizeof name));
+        return false;
+    }
     s->p = t.data_ptr();
     return true;
 }
@@ -228,7 +249,7 @@ bool marshal_all(const Entry &e, PyObject *const *args, Py_ssize_t n, Slot *s) {
     }
     try {
         for (int k = 0; k < e.count; k++)
-            if (!marshal(e, k, args[k], &s[k])) return false;
+            if (!marshal(e, k, args[k], &s[k], s)) return false;
     } catch (const std::exception &x) {
         PyErr_SetString(PyExc_RuntimeError, x.what());
         return false;
@@ -296,14 +317,15 @@ PyObject *py_prepare(PyObject *, PyObject *const *args, Py_ssize_t n) {
     }
     return reinterpret_cast<PyObject *>(p);
 }
-// setup(check, stream_address, CodecCfg, IndexCfg): the callbacks into binding and its struct types
+// setup(check, stream_address, CodecCfg, IndexCfg, MxCfg): the callbacks into binding and its struct types
 PyObject *py_setup(PyObject *, PyObject *const *args, Py_ssize_t n) {
-    if (n != 4 || !PyType_Check(args[2]) || !PyType_Check(args[3]))
-        return PyErr_Format(PyExc_TypeError, "setup(check, stream_address, CodecCfg, IndexCfg)");
+    if (n != 5 || !PyType_Check(args[2]) || !PyType_Check(args[3]) || !PyType_Check(args[4]))
+        return PyErr_Format(PyExc_TypeError, "setup(check, stream_address, CodecCfg, IndexCfg, MxCfg)");
     Py_XSETREF(g_check, Py_NewRef(args[0]));
     Py_XSETREF(g_stream, Py_NewRef(args[1]));
     Py_XSETREF(g_codec_cfg, Py_NewRef(args[2]));
     Py_XSETREF(g_index_cfg, Py_NewRef(args[3]));
+    Py_XSETREF(g_mx_cfg, Py_NewRef(args[4]));
     Py_RETURN_NONE;
 }
 PyMethodDef methods[] = {
