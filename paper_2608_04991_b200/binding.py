@@ -42,7 +42,7 @@ EXPORTS = [
     "rac_recon_error_workspace_bytes", "rac_recon_error",
     "rac_selftest_bounded_wait",
     "rac_mx_record_bytes", "rac_mx_payload_bytes", "rac_mx_encode", "rac_mx_decode", "rac_mx_product",
-    "rac_mx_product_segments",
+    "rac_mx_product_segments", "rac_mx_selftest_bounded_wait",
 ]
 
 
@@ -223,8 +223,10 @@ def load():
     l.rac_mx_encode.argtypes = [mcfgp, vp, i64, vp, sz, vp, vp, vp]
     l.rac_mx_decode.restype = C.c_int
     l.rac_mx_decode.argtypes = [mcfgp, vp, i64, vp, vp, vp]
-    l.rac_mx_product.restype = C.c_int
-    l.rac_mx_product.argtypes = [mcfgp, vp, i64, vp, i64, vp, vp, vp]
+    for name in ("rac_mx_product", "rac_mx_selftest_bounded_wait"):
+        f = getattr(l, name)
+        f.restype = C.c_int
+        f.argtypes = [mcfgp, vp, i64, vp, i64, vp, vp, vp]
     l.rac_mx_product_segments.restype = C.c_int
     l.rac_mx_product_segments.argtypes = [mcfgp, vp, i64, vp, i64, vp, i64, vp, vp, vp]
     from . import _native as native
@@ -463,3 +465,8 @@ def rac_mx_product(cfg, A, M, B, N, Y, dev_status, stream=None) -> None:
 def rac_mx_product_segments(cfg, A, M, seg_off, n_seg, B, N, Y, dev_status, stream=None) -> None:
     """The product with one weight matrix per segment of rows; ``seg_off`` is int32[n_seg + 1] on the device."""
     _calls().rac_mx_product_segments(cfg, A, M, seg_off, n_seg, B, N, Y, dev_status, stream)
+
+
+def rac_mx_selftest_bounded_wait(cfg, A, M, B, N, Y, dev_status, stream=None) -> None:
+    """rac_mx_product with waits that cannot complete; see rac.h."""
+    _calls().rac_mx_selftest_bounded_wait(cfg, A, M, B, N, Y, dev_status, stream)

@@ -111,6 +111,8 @@ const Entry kEntries[] = {
               "cfg,A,M,B,N,Y,dev_status,stream"),
     RAC_ENTRY(rac_mx_product_segments, "mulilulYis",
               "cfg,A,M,seg_off,n_seg,B,N,Y,dev_status,stream"),
+    RAC_ENTRY(rac_mx_selftest_bounded_wait, "mululYis",
+              "cfg,A,M,B,N,Y,dev_status,stream"),
 };
 
 PyObject *g_check = nullptr;   // binding._check(name, return code): raises for a non-zero code

@@ -423,3 +423,22 @@ def test_binding_checks_types_and_devices(env):
         rac.rac_mx_encode(cfg, torch.zeros((64, 2), dtype=torch.float16, device=dev).t(), 2, pay, pay.numel(), None, None)
     rac.rac_mx_encode(cfg, h, 0, pay, 0, None, None)
     rac.rac_mx_product(cfg, pay, 2, pay, 0, torch.empty((2, 0), dtype=torch.float32, device=dev), None)
+
+
+@pytest.mark.parametrize("block", [16, 32])
+@pytest.mark.parametrize("M,N", [(1, 40), (30, 1000), (100, 130), (700, 300)])
+def test_waits_that_cannot_complete_end_with_a_status(env, M, N, block):
+    rac, dev = env.rac, env.dev
+    d = 4096
+    A, a = operand(M, d, block, 1, dev)
+    B, b = operand(N, d, block, 2, dev)
+    cfg = rac.MxCfg(d, block)
+    Y = torch.empty((M, N), dtype=torch.bfloat16, device=dev)
+    status = torch.zeros(1, dtype=torch.int32, device=dev)
+    rac.rac_mx_selftest_bounded_wait(cfg, A, M, B, N, Y, status)
+    torch.cuda.synchronize()
+    assert int(status) == rac.STATUS_TIMEOUT
+    status.zero_()
+    rac.rac_mx_product(cfg, A, M, B, N, Y, status)          # the device is as it was
+    assert int(status) == 0
+    check_product(Y, a, b, torch.bfloat16)
