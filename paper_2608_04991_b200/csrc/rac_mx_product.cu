@@ -2,19 +2,23 @@
 //
 // The tensor cores take the records' codes and block scales as they stand (tcgen05.mma with block scaling, 64 channels an
 // instruction): codes travel by TMA from the records to shared memory in 128-byte swizzled tiles, 256 channels of a row at a
-// time; the scale bytes go through registers, because the tensor cores want the four scales of rows r, r+32, r+64 and r+96
-// beside one another (512-byte atoms, copied to tensor memory by tcgen05.cp).  Sums stay in tensor memory in binary32.  The
-// row exponents of block 16 are powers of two and commute with the sum: the epilogue applies them.
+// time, scale bytes by TMA too; four warps, one for each quarter of tensor memory's lanes, carry the scales from shared to
+// tensor memory (tcgen05.st), where lane i holds beside one another the scales of rows i, i+32, i+64 and i+96.  The
+// copy instruction made for this (tcgen05.cp) takes its turn between the matrix instructions and held them up: 384 us
+// against 220 us without any scales for 16384 x 5120 x 5120.  Sums stay in tensor memory in binary32.  The row exponents of
+// block 16 are powers of two and commute with the sum: the epilogue applies them.
 //
-// One pipeline, two shapes of work.
-//   wide    many rows: a tile is 128 rows of A by 256 of B; rows of A are the lanes of the accumulator, so a thread holds
-//           consecutive values of a row of Y.  Persistent CTAs, one per SM.
+// Two shapes of work.
+//   wide    many rows: a pair of CTAs makes a tile of 256 rows of A by 256 (128) of B with cta_group::2, so that each CTA loads
+//           half of either operand.  Rows of A are the lanes of the accumulator: a thread holds consecutive values of a row
+//           of Y.  Persistent pairs.  What bounds it is the way from L2 to shared memory: 128 x 256 tiles of single CTAs
+//           (54 KB for what is 38 KB per CTA here) took 214 us with all but one of every four matrix instructions left out.
 //   narrow  few rows (a decode step, a segment of a few tokens): a tile is 128 rows of B by up to 128 of A, so the weights
 //           fill the 128 lanes and a handful of tokens costs a handful of columns.  What bounds it is reading the weights;
 //           where the tiles alone do not fill the SMs, clusters split the channels and add their partial sums through
 //           distributed shared memory in a fixed order.
-// Warps 0-3 of a CTA are the epilogue, 4 issues TMA loads, 5 the matrix instructions, 6 and up carry scales.  Every wait on
-// an mbarrier is bounded: a copy that never lands ends the kernel with RAC_STATUS_TIMEOUT.
+// Warps 0-3 of a CTA are the epilogue, 4-7 (wide: 4-11) carry scales, the next issues TMA loads and the last the matrix
+// instructions.  Every wait on an mbarrier is bounded: a copy that never lands ends the kernel with RAC_STATUS_TIMEOUT.
 #include <cuda.h>
 
 #include "rac_mx.cuh"
@@ -22,7 +26,8 @@
 namespace rac {
 
 constexpr int kStageK = 256;             // channels per pipeline stage: one 128-byte row of codes
-constexpr int kPRows = 128;              // rows of the operand that fills the accumulator's lanes
+constexpr int kRows = 128;               // lanes of an accumulator
+constexpr int kNarrowThreads = 320, kWideThreads = 448;
 
 struct MxProductParams {
     const uint8_t *A, *B;
@@ -34,8 +39,14 @@ struct MxProductParams {
     int d, rec, scale_off, nblk, y_type;
     int k_stages;             // ceil(d / 256)
     int n_tiles;              // tiles along N
-    int split;                // CTAs of a cluster that share the channels of a tile (narrow), 1 = none
+    int split;                // narrow: CTAs of a cluster that share the channels of a tile, 1 = none
+    int y_maps;               // wide: Y has rows that TMA can store
     uint32_t test_extra_tx;   // rac_mx_selftest_bounded_wait: bytes announced beyond what a stage's copies deliver
+};
+struct MxMaps {
+    CUtensorMap a, b;              // codes
+    CUtensorMap a_scale, b_scale;
+    CUtensorMap y;
 };
 
 // ------------------------------------------------------------------------------------------------ PTX
@@ -44,90 +55,133 @@ __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap *map
                  ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar)
                  : "memory");
 }
+__device__ __forceinline__ void tma_store_2d(const CUtensorMap *map, int x, int y, uint32_t src) {
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(x), "r"(y), "r"(src)
+                 : "memory");
+}
+__device__ __forceinline__ void tma_prefetch(const CUtensorMap *map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
 __device__ __forceinline__ void mbar_arrive(uint32_t bar) {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
-__device__ __forceinline__ void tc_commit(uint32_t bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+// Arrival on the barrier at the same place in the cluster's CTA `rank`, and the wait for such arrivals.  What they announce is
+// complete when they are made (copies that have landed, stores to tensor memory that were waited for, tensor memory that was
+// read) and no ordinary memory passes between the CTAs by them, so they carry no ordering of the whole cluster's memory:
+// with .release.cluster and .acquire.cluster 16384 x 5120 x 5120 took 411 us, without 220 us.
+__device__ __forceinline__ void mbar_arrive_at(uint32_t bar, uint32_t rank) {
+    asm volatile("{\n\t.reg .b32 far;\n\tmapa.shared::cluster.u32 far, %0, %1;\n\t"
+                 "mbarrier.arrive.shared::cluster.b64 _, [far];\n\t}" ::"r"(bar), "r"(rank)
+                 : "memory");
+}
+// all threads of the cluster
+__device__ __forceinline__ void cluster_barrier() {
+    asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
+}
+// a word of the shared memory of the cluster's CTA `rank`, at the place `addr` has in this one's
+__device__ __forceinline__ uint32_t cluster_load(uint32_t addr, uint32_t rank) {
+    uint32_t v;
+    asm volatile("{\n\t.reg .b32 far;\n\tmapa.shared::cluster.u32 far, %1, %2;\n\tld.shared::cluster.u32 %0, [far];\n\t}"
+                 : "=r"(v) : "r"(addr), "r"(rank));
+    return v;
 }
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-// 512 bytes of scales (32 rows of 16) to 4 columns of tensor memory, the same in all four groups of 32 lanes
-__device__ __forceinline__ void tc_copy_scales(uint32_t tmem, uint64_t desc) {
-    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
+
+// PAIR: instructions for two CTAs at once, issued by the cluster's first; what they commit arrives at both
+template <bool PAIR>
+__device__ __forceinline__ void tc_commit(uint32_t bar) {
+    if constexpr (PAIR)
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                     ::"r"(bar), "h"(static_cast<uint16_t>(3)) : "memory");
+    else
+        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
-template <int BLOCK>
+#define RAC_TC_MMA(group, kind)                                                                                    \
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %6, 0;\n\t"                                               \
+                 "tcgen05.mma.cta_group::" group ".kind::" kind " [%0], %1, %2, %3, [%4], [%5], p;\n\t}"           \
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(static_cast<uint32_t>(add))           \
+                 : "memory")
+template <int BLOCK, bool PAIR>
 __device__ __forceinline__ void tc_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb, bool add) {
     if constexpr (BLOCK == 16) {
-        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %6, 0;\n\t"
-                     "tcgen05.mma.cta_group::1.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
-                     ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(static_cast<uint32_t>(add))
-                     : "memory");
+        if constexpr (PAIR) RAC_TC_MMA("2", "mxf4nvf4.block_scale.scale_vec::4X");
+        else RAC_TC_MMA("1", "mxf4nvf4.block_scale.scale_vec::4X");
     } else {
-        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %6, 0;\n\t"
-                     "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
-                     ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(static_cast<uint32_t>(add))
-                     : "memory");
+        if constexpr (PAIR) RAC_TC_MMA("2", "mxf4.block_scale.scale_vec::2X");
+        else RAC_TC_MMA("1", "mxf4.block_scale.scale_vec::2X");
     }
 }
-// 16 columns of this thread's lane
-__device__ __forceinline__ void tc_load16(uint32_t tmem, float (&v)[16]) {
-    uint32_t r[16];
+// Shared-memory descriptor of codes: rows of 128 bytes, 128-byte swizzle (2 in the top three bits), 1024 bytes from one group of
+// eight rows to the next (addresses and offsets in units of 16 bytes, version 1 in bit 46).
+__device__ __forceinline__ uint64_t desc_codes(uint32_t addr) {
+    return static_cast<uint64_t>((addr & 0x3ffffu) >> 4) | 1ull << 16 | 64ull << 32 | 1ull << 46 | 2ull << 61;
+}
+// Instruction descriptor: both operands e2m1 and K-major, m rows by n; scales e4m3 or e8m0; `half`: which two of the four
+// scale bytes of a column (block 32).
+template <int BLOCK>
+__device__ __forceinline__ uint32_t instr_desc(int m, int n, int half) {
+    return static_cast<uint32_t>(2 * half) << 4 | 1u << 7 | 1u << 10 | static_cast<uint32_t>(n >> 3) << 17 | (BLOCK == 32 ? 1u << 23 : 0u) |
+           static_cast<uint32_t>(m >> 7) << 27 | static_cast<uint32_t>(2 * half) << 29;
+}
+
+// the matrix instructions of one stage: `n` (4, except at the end of a row) times 64 channels
+template <int BLOCK, bool PAIR, int QROWS, int QCOLS>
+__device__ __forceinline__ void tc_stage(int n, uint32_t d, uint64_t a, uint64_t b, uint32_t sa, uint32_t sb, bool add) {
+    auto one = [&](int j) {
+        const int word = BLOCK == 16 ? j : j / 2, half = BLOCK == 16 ? 0 : j & 1;
+        tc_mma<BLOCK, PAIR>(d, a + 2 * j, b + 2 * j, instr_desc<BLOCK>(PAIR ? 256 : 128, QROWS, half), sa + 4 * word, sb + QCOLS * word, add || j > 0);
+    };
+    if (n == 4) {        // written out: this thread keeps the tensor cores busy, and a loop with its descriptors costs 160 cycles a stage
+        one(0);
+        one(1);
+        one(2);
+        one(3);
+    } else {
+        for (int j = 0; j < n; j++) one(j);
+    }
+}
+template <bool PAIR, int COLUMNS>
+__device__ __forceinline__ void tc_alloc(uint32_t at) {
+    if constexpr (PAIR) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(at), "n"(COLUMNS) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    } else {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(at), "n"(COLUMNS) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+}
+template <bool PAIR, int COLUMNS>
+__device__ __forceinline__ void tc_free(uint32_t tmem) {
+    if constexpr (PAIR) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(COLUMNS) : "memory");
+    else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(COLUMNS) : "memory");
+}
+// 16 columns of this thread's lane; `wait` before they are looked at
+__device__ __forceinline__ void tc_load16(uint32_t tmem, uint32_t (&r)[16]) {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
                    "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
                  : "r"(tmem));
-    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-#pragma unroll
-    for (int i = 0; i < 16; i++) v[i] = __uint_as_float(r[i]);
 }
-
-// Shared-memory descriptors (address and offsets in units of 16 bytes, version 1 in bit 46).
-// Codes: rows of 128 bytes, 128-byte swizzle (2 in the top three bits), 1024 bytes from one group of eight rows to the next.
-__device__ __forceinline__ uint64_t desc_codes(uint32_t addr) {
-    return static_cast<uint64_t>((addr & 0x3ffffu) >> 4) | 1ull << 16 | 64ull << 32 | 1ull << 46 | 2ull << 61;
+__device__ __forceinline__ void tc_load_wait(uint32_t (&r)[16]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]),
+                   "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
+                 :: "memory");
 }
-// Scales: no swizzle, 128 bytes from one group of eight rows (of 16 bytes) to the next.
-__device__ __forceinline__ uint64_t desc_scales(uint32_t addr) {
-    return static_cast<uint64_t>((addr & 0x3ffffu) >> 4) | 8ull << 16 | 8ull << 32 | 1ull << 46;
+template <int N>
+__device__ __forceinline__ void tc_store(uint32_t tmem, const uint32_t *r) {
+    static_assert(N == 8 || N == 16, "columns");
+    if constexpr (N == 8)
+        asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+                     ::"r"(tmem), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
+    else
+        asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
+                     ::"r"(tmem), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
+                       "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
 }
-// Instruction descriptor: both operands e2m1 and K-major, 128 rows by n; scales e4m3 or e8m0; `half`: which two of the four
-// scale bytes of a column (block 32).
-template <int BLOCK>
-__device__ __forceinline__ uint32_t instr_desc(int n, int half) {
-    return static_cast<uint32_t>(2 * half) << 4 | 1u << 7 | 1u << 10 | static_cast<uint32_t>(n >> 3) << 17 | (BLOCK == 32 ? 1u << 23 : 0u) |
-           1u << 27 | static_cast<uint32_t>(2 * half) << 29;
-}
-
-// ------------------------------------------------------------------------------------------------ layout
-template <int BLOCK, int QROWS>
-struct MxLayout {
-    static constexpr bool kWide = QROWS == 256;
-    static constexpr int kAtoms = BLOCK == 16 ? 4 : 2;                 // scale atoms per stage and 128 rows
-    static constexpr int kQGroups = kWide ? 2 : 1;                     // groups of 128 rows of Q
-    static constexpr int kP = kPRows * 128, kQ = QROWS * 128;          // bytes of codes
-    static constexpr int kScales = (1 + kQGroups) * kAtoms * 512;
-    static constexpr int kStage = kP + kQ + kScales;
-    static constexpr int kStages = QROWS == 128 || QROWS == 64 ? 3 : 4;
-    static constexpr int kCtrl = 256;
-    static constexpr int kExtra = kWide ? 1024 + 4 * 32 * 17 * 4 : 0;  // factors of Q's rows, transposition of odd rows of Y
-    static constexpr int kBytes = 1024 + kCtrl + kStages * kStage + kExtra;      // 1024: alignment of the tiles
-    static constexpr int kScaleCols = (1 + kQGroups) * kAtoms * 4;     // columns of tensor memory per stage
-    static constexpr int kColumns = kWide ? 512 : 256;
-    static constexpr int kScaleBase = kWide ? 256 : 128;
-    static constexpr int kThreads = 32 * (6 + 1 + kQGroups);
-    static_assert(kScaleBase + kStages * kScaleCols <= kColumns, "tensor memory");
-    static_assert(kBytes <= 227 * 1024 && (kWide || (kBytes > 77 * 1024 && kBytes <= 113 * 1024)),
-                  "narrow: two CTAs an SM and no third, whose columns would not fit");
-};
-struct MxCtrl {
-    unsigned long long full_codes[4], full_scales[4], empty[4], acc_full, acc_empty;
-    uint32_t tmem;
-    int abort;
-};
+__device__ __forceinline__ void tc_store_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 // ------------------------------------------------------------------------------------------------ tiles
-// The rows of tile `t` (all the rows of a warp call this together, with t never falling).
+// The rows of tile `t` (all lanes of a warp call this together, with t never falling).
 struct Tile {
     int64_t lo, hi;     // rows of A that are left of the segment, from the tile's first
     int64_t matrix;     // first row of B of the segment's matrix
@@ -184,54 +238,38 @@ struct TileWalk {
 };
 
 // ------------------------------------------------------------------------------------------------ scales
-// The scale bytes of 128 rows and one stage: lane i holds those of rows i, i+32, i+64, i+96.
 template <int BLOCK>
-struct ScaleChunk {
-    uint4 v[4];
-    __device__ __forceinline__ void load(const uint8_t *recs, int64_t row0, int64_t rows, int stage, const MxProductParams &p) {
-        constexpr int kBytes = kStageK / BLOCK;
-        const int left = p.nblk - stage * kBytes;          // what lies behind the scales is not one
-#pragma unroll
-        for (int i = 0; i < 4; i++) {
-            const int64_t row = row0 + (threadIdx.x & 31) + 32 * i;
-            v[i] = make_uint4(0, 0, 0, 0);
-            if (row < rows) {
-                const uint8_t *src = recs + row * p.rec + p.scale_off + stage * kBytes;
-                if (BLOCK == 16) {
-                    v[i] = *reinterpret_cast<const uint4 *>(src);
-                } else {
-                    const uint2 w = *reinterpret_cast<const uint2 *>(src);
-                    v[i].x = w.x;
-                    v[i].y = w.y;
-                }
-                if (left < kBytes) {
-                    uint32_t *w = &v[i].x;
-#pragma unroll
-                    for (int j = 0; j < kBytes / 4; j++) {
-                        const int n = left - 4 * j;
-                        w[j] &= n >= 4 ? 0xffffffffu : n <= 0 ? 0u : (1u << (8 * n)) - 1u;
-                    }
-                }
-                if (BLOCK == 16) {
-                    v[i].x &= 0x7f7f7f7fu;
-                    v[i].y &= 0x7f7f7f7fu;
-                    v[i].z &= 0x7f7f7f7fu;
-                    v[i].w &= 0x7f7f7f7fu;
-                }
-            }
-        }
-    }
-    // atom j: 16 bytes per lane, the four scales of each of its four rows
-    __device__ __forceinline__ void store(uint32_t smem) const {
-        const uint32_t at = smem + (threadIdx.x & 31) * 16;
-        sts128(at, make_uint4(v[0].x, v[1].x, v[2].x, v[3].x));
-        sts128(at + 512, make_uint4(v[0].y, v[1].y, v[2].y, v[3].y));
-        if (BLOCK == 16) {
-            sts128(at + 1024, make_uint4(v[0].z, v[1].z, v[2].z, v[3].z));
-            sts128(at + 1536, make_uint4(v[0].w, v[1].w, v[2].w, v[3].w));
-        }
-    }
+struct Scales {
+    static constexpr int kWords = BLOCK == 16 ? 4 : 2;     // words of a row per stage: four scales each
+    static constexpr int kBytes = 4 * kWords;
 };
+// The scales of one stage and 128 rows to tensor memory: word j of row i + 32g to lane i, column 4j + g (times `stride` / 4).
+// `at`: where this lane finds the words of row i; `next`: from there to row i + 32.  What lies behind a row's scales (`left`
+// of them from the stage's first) counts as 0, and so does bit 7 of an e4m3 scale.
+template <int BLOCK, int GROUPS>
+__device__ __forceinline__ void load_scales(uint32_t (&w)[Scales<BLOCK>::kWords * 4], uint32_t at, uint32_t next, int left) {
+    constexpr int kWords = Scales<BLOCK>::kWords;
+#pragma unroll
+    for (int g = 0; g < 4; g++) {
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (g < GROUPS) {
+            if constexpr (BLOCK == 16) v = lds128(at + g * next);
+            else asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at + g * next));
+        }
+        const uint32_t vs[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int j = 0; j < kWords; j++) w[4 * j + g] = BLOCK == 16 ? vs[j] & 0x7f7f7f7fu : vs[j];
+    }
+    if (left < Scales<BLOCK>::kBytes) {
+#pragma unroll
+        for (int j = 0; j < kWords; j++) {
+            const int n = left - 4 * j;
+            const uint32_t mask = n >= 4 ? 0xffffffffu : n <= 0 ? 0u : (1u << (8 * n)) - 1u;
+#pragma unroll
+            for (int g = 0; g < 4; g++) w[4 * j + g] &= mask;
+        }
+    }
+}
 
 // ------------------------------------------------------------------------------------------------ results
 __device__ __forceinline__ void store_y(const MxProductParams &p, int64_t at, float v) {
@@ -239,61 +277,50 @@ __device__ __forceinline__ void store_y(const MxProductParams &p, int64_t at, fl
     else if (p.y_type == RAC_MX_FP16) static_cast<__half *>(p.Y)[at] = __float2half_rn(v);
     else static_cast<__nv_bfloat16 *>(p.Y)[at] = __float2bfloat16_rn(v);
 }
-// 16 consecutive values of a row of Y, at an address that is a multiple of 16 bytes
-__device__ __forceinline__ void store_y16(const MxProductParams &p, int64_t at, const float (&v)[16]) {
-    if (p.y_type == RAC_MX_FP32) {
-        float4 *dst = reinterpret_cast<float4 *>(static_cast<float *>(p.Y) + at);
-#pragma unroll
-        for (int i = 0; i < 4; i++) dst[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
-        return;
+// v times 2^e, rounded once (a factor of its own may be beyond binary32)
+__device__ __forceinline__ float scaled(float v, int e) { return e >= -126 && e <= 126 ? v * mx_pow2(e) : ldexpf(v, e); }
+__device__ __forceinline__ uint32_t pack16(int y_type, float lo, float hi) {
+    if (y_type == RAC_MX_FP16) {
+        const __half2 h = __floats2half2_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t *>(&h);
     }
-    uint32_t w[8];
-#pragma unroll
-    for (int i = 0; i < 8; i++) {
-        if (p.y_type == RAC_MX_FP16) {
-            const __half2 h = __floats2half2_rn(v[2 * i], v[2 * i + 1]);
-            w[i] = *reinterpret_cast<const uint32_t *>(&h);
-        } else {
-            w[i] = f2_to_bf16x2(v[2 * i], v[2 * i + 1]);
-        }
-    }
-    uint4 *dst = reinterpret_cast<uint4 *>(static_cast<uint16_t *>(p.Y) + at);
-    dst[0] = make_uint4(w[0], w[1], w[2], w[3]);
-    dst[1] = make_uint4(w[4], w[5], w[6], w[7]);
+    return f2_to_bf16x2(lo, hi);
 }
 
-// all threads of the cluster
-__device__ __forceinline__ void cluster_barrier() {
-    asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
-}
-// a word of the shared memory of the cluster's CTA `rank`, at the place `addr` has in this one's
-__device__ __forceinline__ uint32_t cluster_load(uint32_t addr, int rank) {
-    uint32_t far, v;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(far) : "r"(addr), "r"(rank));
-    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(far) : "memory");
-    return v;
-}
-__device__ __forceinline__ void epilogue_barrier() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
+// ------------------------------------------------------------------------------------------------ narrow
+template <int QROWS>
+struct NarrowLayout {
+    static constexpr int kP = kRows * 128, kQ = QROWS * 128, kPScale = kRows * 16, kQScale = QROWS * 16;   // bytes
+    static constexpr int kTx = kP + kQ + kPScale + kQScale;
+    static constexpr int kStage = (kTx + 1023) / 1024 * 1024;
+    static constexpr int kStages = QROWS == 128 ? 3 : QROWS == 64 ? 4 : 5;
+    static constexpr int kBytes = 1024 + kStages * kStage + 256;             // 1024: alignment of the tiles
+    static constexpr int kGroups = QROWS > 32 ? QROWS / 32 : 1;              // groups of 32 rows of Q
+    static constexpr int kColumns = 256, kScaleBase = QROWS == 128 ? 128 : 64, kScaleCols = 32;
+    static_assert(kScaleBase + kStages * kScaleCols <= kColumns, "tensor memory");
+    static_assert(kBytes > 77 * 1024 && kBytes <= 113 * 1024, "two CTAs an SM and no third, whose columns would not fit");
+};
+struct NarrowCtrl {
+    unsigned long long full[5], ready[5], empty[5], acc_full, acc_empty;
+    uint32_t tmem;
+    int abort;
+};
 
-// ------------------------------------------------------------------------------------------------ the kernel
 template <int BLOCK, int QROWS>
-__global__ void __launch_bounds__(MxLayout<BLOCK, QROWS>::kThreads, MxLayout<BLOCK, QROWS>::kWide ? 1 : 2)
-    mx_product_kernel(const MxProductParams p, const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b) {
-    using L = MxLayout<BLOCK, QROWS>;
-    constexpr bool kWide = L::kWide;
-    constexpr int MROWS = kWide ? kPRows : QROWS, NROWS = kWide ? QROWS : kPRows;
+__global__ void __launch_bounds__(kNarrowThreads, 2) mx_narrow_kernel(const MxProductParams p, const __grid_constant__ MxMaps maps) {
+    using L = NarrowLayout<QROWS>;
+    constexpr int kWords = Scales<BLOCK>::kWords;
     extern __shared__ uint8_t raw[];
     const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
     uint8_t *const base_ptr = raw + (base - smem_u32(raw));
-    const uint32_t stage0 = base, ctrl_at = base + L::kStages * L::kStage;
-    MxCtrl *ctrl = reinterpret_cast<MxCtrl *>(base_ptr + L::kStages * L::kStage);
+    NarrowCtrl *ctrl = reinterpret_cast<NarrowCtrl *>(base_ptr + L::kStages * L::kStage);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    auto bar = [&](const unsigned long long *b) { return ctrl_at + static_cast<uint32_t>(reinterpret_cast<const uint8_t *>(b) - reinterpret_cast<const uint8_t *>(ctrl)); };
+    auto bar = [&](const unsigned long long *b) { return smem_u32(b); };
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < L::kStages; i++) {
-            mbar_init(bar(&ctrl->full_codes[i]), 1);
-            mbar_init(bar(&ctrl->full_scales[i]), 1 + L::kQGroups);
+            mbar_init(bar(&ctrl->full[i]), 1);
+            mbar_init(bar(&ctrl->ready[i]), 4);
             mbar_init(bar(&ctrl->empty[i]), 1);
         }
         mbar_init(bar(&ctrl->acc_full), 1);
@@ -301,10 +328,8 @@ __global__ void __launch_bounds__(MxLayout<BLOCK, QROWS>::kThreads, MxLayout<BLO
         ctrl->abort = 0;
         mbar_init_fence();
     }
-    if (warp == 5) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ctrl->tmem)), "n"(L::kColumns) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-    }
+    if (warp == 8 && lane < 4) tma_prefetch(&maps.a + lane);
+    if (warp == 9) tc_alloc<false, L::kColumns>(smem_u32(&ctrl->tmem));
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -321,13 +346,14 @@ __global__ void __launch_bounds__(MxLayout<BLOCK, QROWS>::kThreads, MxLayout<BLO
         *reinterpret_cast<volatile int *>(&ctrl->abort) = 1;
     };
     auto aborted = [&]() { return *reinterpret_cast<volatile int *>(&ctrl->abort) != 0; };
-    TileWalk<MROWS, NROWS> walk, walk_sum;
+    TileWalk<QROWS, kRows> walk, walk_sum;
     int it = 0, done = 0;       // stages and tiles that this role has gone through
+    const int exp_off = p.scale_off + p.nblk;
 
     // Without split one pass of this loop, in which every role goes through all of the CTA's tiles; with split one per tile.
     for (int64_t t0 = first;; t0 += step) {
-        if (warp == 4) {
-            // ---- codes: TMA
+        if (warp == 8) {
+            // ---- TMA
             bool ok = true;
             for (int64_t t = t0; ok; t += step) {
                 const Tile tile = walk.at(p, t);
@@ -341,22 +367,25 @@ __global__ void __launch_bounds__(MxLayout<BLOCK, QROWS>::kThreads, MxLayout<BLO
                             ok = false;
                             break;
                         }
-                        const uint32_t full = bar(&ctrl->full_codes[st]), dst = stage0 + st * L::kStage;
-                        mbar_arrive_expect_tx(full, L::kP + L::kQ + p.test_extra_tx);
-                        tma_load_2d(dst, kWide ? &map_a : &map_b, ks * 128, kWide ? row_a : row_b, full);
-                        tma_load_2d(dst + L::kP, kWide ? &map_b : &map_a, ks * 128, kWide ? row_b : row_a, full);
+                        const uint32_t full = bar(&ctrl->full[st]), dst = base + st * L::kStage;
+                        const int xs = BLOCK == 16 ? ks * 16 : ks / 2 * 16;       // block 32: 16 bytes are two stages' scales
+                        mbar_arrive_expect_tx(full, L::kTx + p.test_extra_tx);
+                        tma_load_2d(dst, &maps.b, ks * 128, row_b, full);
+                        tma_load_2d(dst + L::kP, &maps.a, ks * 128, row_a, full);
+                        tma_load_2d(dst + L::kP + L::kQ, &maps.b_scale, xs, row_b, full);
+                        tma_load_2d(dst + L::kP + L::kQ + L::kPScale, &maps.a_scale, xs, row_a, full);
                     }
                 }
                 ok = __shfl_sync(0xffffffffu, ok, 0);
                 if (split > 1) break;
             }
             if (!ok && lane == 0) {      // copies in flight must land before the CTA's memory is given back
-                for (int i = max(0, it - L::kStages); i < it; i++) mbar_wait_bounded(bar(&ctrl->full_codes[i % L::kStages]), i / L::kStages & 1);
+                for (int i = max(0, it - L::kStages); i < it; i++) mbar_wait_bounded(bar(&ctrl->full[i % L::kStages]), i / L::kStages & 1);
             }
-        } else if (warp == 5) {
+        } else if (warp == 9) {
             // ---- matrix instructions
             bool ok = true;
-            for (int64_t t = t0; ok; t += step, done++) {
+            for (int64_t t = t0; ok; t += step) {
                 const Tile tile = walk.at(p, t);
                 if (!tile.valid) break;
                 if (lane == 0) {
@@ -365,162 +394,79 @@ __global__ void __launch_bounds__(MxLayout<BLOCK, QROWS>::kThreads, MxLayout<BLO
                     for (int ks = ks0; ok && ks < ks1; ks++, it++) {
                         const int st = it % L::kStages;
                         const uint32_t phase = it / L::kStages & 1;
-                        ok = mbar_wait_bounded(bar(&ctrl->full_codes[st]), phase) && mbar_wait_bounded(bar(&ctrl->full_scales[st]), phase) && !aborted();
+                        ok = mbar_wait_bounded(bar(&ctrl->full[st]), phase) && mbar_wait_bounded(bar(&ctrl->ready[st]), phase) && !aborted();
                         if (!ok) break;
                         tc_fence_after();
-                        const uint32_t at = stage0 + st * L::kStage;
-                        const uint32_t sp = tmem + L::kScaleBase + st * L::kScaleCols, sq = sp + L::kAtoms * 4;
-                        const int mmas = min(4, (p.d - ks * kStageK + 63) / 64), atoms = BLOCK == 16 ? mmas : (mmas + 1) / 2;
-                        const uint64_t ds = desc_scales(at + L::kP + L::kQ);
-                        for (int j = 0; j < atoms; j++) {
-                            tc_copy_scales(sp + 4 * j, ds + j * 32);
-#pragma unroll
-                            for (int g = 0; g < L::kQGroups; g++)
-                                tc_copy_scales(sq + (j * L::kQGroups + g) * 4, ds + ((1 + g) * L::kAtoms + j) * 32);
-                        }
-                        const uint64_t dp = desc_codes(at), dq = desc_codes(at + L::kP);
-                        for (int j = 0; j < mmas; j++) {
-                            const int atom = BLOCK == 16 ? j : j / 2, half = BLOCK == 16 ? 0 : j & 1;
-                            tc_mma<BLOCK>(tmem, dp + 2 * j, dq + 2 * j, instr_desc<BLOCK>(QROWS, half), sp + 4 * atom,
-                                          sq + 4 * L::kQGroups * atom, ks > ks0 || j > 0);
-                        }
-                        tc_commit(bar(&ctrl->empty[st]));
+                        const uint32_t sp = tmem + L::kScaleBase + st * L::kScaleCols, sq = sp + 16;
+                        const uint64_t dp = desc_codes(base + st * L::kStage), dq = desc_codes(base + st * L::kStage + L::kP);
+                        tc_stage<BLOCK, false, QROWS, 4>(min(4, (p.d - ks * kStageK + 63) / 64), tmem, dp, dq, sp, sq, ks > ks0);
+                        tc_commit<false>(bar(&ctrl->empty[st]));
                     }
-                    if (ok) tc_commit(bar(&ctrl->acc_full));
-                    else {
-                        give_up();                         // what was issued ends before its operands and sums are given back
-                        tc_commit(bar(&ctrl->acc_full));
-                        mbar_wait_bounded(bar(&ctrl->acc_full), done & 1);
-                    }
+                    if (!ok) give_up();
+                    tc_commit<false>(bar(&ctrl->acc_full));
+                    // what was issued ends before its operands and sums are given back
+                    if (!ok) mbar_wait_bounded(bar(&ctrl->acc_full), done & 1);
                 }
+                done++;
                 ok = __shfl_sync(0xffffffffu, ok, 0);
-                if (split > 1) {
-                    done++;
-                    break;
-                }
+                if (split > 1) break;
             }
-        } else if (warp >= 6) {
-            // ---- scales: warp 6 those of P, the others those of Q, four stages ahead in registers
-            const int part = warp - 6;
-            const uint8_t *recs = (part == 0) == kWide ? p.A : p.B;
-            ScaleChunk<BLOCK> chunk[4];
-            int64_t t = t0;
-            Tile tile = walk.at(p, t);
-            int ks = ks0, loaded = 0, stored = 0;
-            auto fetch = [&](ScaleChunk<BLOCK> &c) {
-                if (!tile.valid) return;
-                const bool of_a = (part == 0) == kWide;
-                const int64_t row0 = of_a ? tile.lo : tile.matrix + tile.n0 + (part > 0 ? 128 * (part - 1) : 0);
-                const int64_t rows = of_a ? min(tile.hi, tile.lo + MROWS) : tile.matrix + p.N;
-                c.load(recs, row0, rows, ks, p);
-                loaded++;
-                if (++ks == ks1) {
-                    ks = ks0;
-                    t += step;
-                    if (split > 1) tile.valid = false;
-                    else tile = walk.at(p, t);
-                }
-            };
+        } else if (warp >= 4) {
+            // ---- scales, a quarter of the lanes each
+            const uint32_t quarter = static_cast<uint32_t>(32 * (warp - 4)) << 16;
             bool ok = true;
-#pragma unroll
-            for (int j = 0; j < 3; j++) fetch(chunk[j]);
-            while (ok && stored < loaded) {
-#pragma unroll
-                for (int j = 0; j < 4; j++) {
-                    if (!ok || stored >= loaded) break;
-                    fetch(chunk[(j + 3) & 3]);
+            for (int64_t t = t0; ok; t += step) {
+                const Tile tile = walk.at(p, t);
+                if (!tile.valid) break;
+                for (int ks = ks0; ks < ks1; ks++, it++) {
                     const int st = it % L::kStages;
-                    ok = mbar_wait_bounded(bar(&ctrl->empty[st]), (it / L::kStages & 1) ^ 1) && !aborted();
+                    ok = mbar_wait_bounded(bar(&ctrl->full[st]), it / L::kStages & 1) && !aborted();
                     ok = __all_sync(0xffffffffu, ok);
                     if (!ok) break;
-                    chunk[j].store(stage0 + st * L::kStage + L::kP + L::kQ + part * L::kAtoms * 512);
-                    fence_async_smem();
+                    tc_fence_after();
+                    const uint32_t at = base + st * L::kStage + L::kP + L::kQ + (BLOCK == 32 ? 8 * (ks & 1) : 0);
+                    const int left = p.nblk - ks * Scales<BLOCK>::kBytes;
+                    uint32_t wp[kWords * 4], wq[kWords * 4];
+                    load_scales<BLOCK, 4>(wp, at + lane * 16, 512, left);
+                    load_scales<BLOCK, L::kGroups>(wq, at + L::kPScale + (lane & (QROWS - 1)) * 16, 512, left);
+                    const uint32_t to = tmem + quarter + L::kScaleBase + st * L::kScaleCols;
+                    tc_store<kWords * 4>(to, wp);
+                    tc_store<kWords * 4>(to + 16, wq);
+                    tc_store_wait();
+                    tc_fence_before();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(bar(&ctrl->full_scales[st]));
-                    it++;
-                    stored++;
+                    if (lane == 0) mbar_arrive(bar(&ctrl->ready[st]));
                 }
+                if (split > 1) break;
             }
             if (!ok && lane == 0) give_up();
         } else if (split == 1) {
-            // ---- epilogue: warps 0-3, 32 lanes of the accumulator each
-            float *const factor = reinterpret_cast<float *>(base_ptr + L::kStages * L::kStage + L::kCtrl);
+            // ---- epilogue, 32 lanes of the accumulator each: lanes are rows of B, 32 consecutive values of a row of Y per warp
             const uint32_t acc = tmem + (static_cast<uint32_t>(32 * warp) << 16);
-            const int exp_off = p.scale_off + p.nblk;
+            const int r = 32 * warp + lane;
             bool ok = true;
             for (int64_t t = t0; ok; t += step, done++) {
                 const Tile tile = walk.at(p, t);
                 if (!tile.valid) break;
-                const int64_t rows = min(tile.hi - tile.lo, static_cast<int64_t>(MROWS)), cols = min(p.N - tile.n0, static_cast<int64_t>(NROWS));
-                const uint8_t *a = p.A + tile.lo * p.rec + exp_off, *b = p.B + (tile.matrix + tile.n0) * p.rec + exp_off;
-                const int r = 32 * warp + lane;            // this thread's lane of the accumulator
-                int e = 0;
-                bool plain = true;                         // exponents so small that their factors multiply without loss
-                if (kWide && BLOCK == 16) {
-                    epilogue_barrier();                    // the tile before has read its factors
-                    e = r < rows ? mx_row_exp(a + r * static_cast<int64_t>(p.rec), 0) : 0;
-                    for (int c = r; c < NROWS; c += 128) {
-                        const int eb = c < cols ? mx_row_exp(b + c * static_cast<int64_t>(p.rec), 0) : 0;
-                        reinterpret_cast<int *>(factor)[c] = eb;
-                        plain = plain && eb >= -50 && eb <= 50;
-                    }
-                    plain = plain && e >= -50 && e <= 50;
-                    uint32_t all;
-                    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbar.red.and.pred q, 1, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
-                                 : "=r"(all) : "r"(static_cast<uint32_t>(plain)) : "memory");
-                    plain = all != 0;
-                } else if (BLOCK == 16) {
-                    e = r < cols ? mx_row_exp(b + r * static_cast<int64_t>(p.rec), 0) : 0;
-                }
+                const int rows = static_cast<int>(min(tile.hi - tile.lo, static_cast<int64_t>(QROWS)));
+                const int cols = static_cast<int>(min(p.N - tile.n0, static_cast<int64_t>(kRows)));
+                const uint8_t *a = p.A + tile.lo * p.rec, *b = p.B + (tile.matrix + tile.n0) * p.rec;
+                const int eb = BLOCK == 16 && r < cols ? mx_row_exp(b + r * static_cast<int64_t>(p.rec), exp_off) : 0;
                 ok = mbar_wait_bounded(bar(&ctrl->acc_full), done & 1) && !aborted();
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 tc_fence_after();
-                if constexpr (kWide) {
-                    const int esize = p.y_type == RAC_MX_FP32 ? 4 : 2;
-                    const bool straight = p.N * esize % 16 == 0;
-                    float *const turn = factor + 256 + warp * 32 * 17;
-                    const float fa = plain ? mx_pow2(e) : 0.0f;
-                    for (int c = 0; c < cols; c += 16) {
-                        float v[16];
-                        tc_load16(acc + c, v);
-                        if (BLOCK == 16) {
-                            const int4 *eb = reinterpret_cast<const int4 *>(factor + c);
+                for (int c = 0; c < rows; c += 16) {
+                    uint32_t v[16];
+                    tc_load16(acc + c, v);
+                    const int m = c + (lane & 15);
+                    const int ea = BLOCK == 16 && m < rows ? mx_row_exp(a + m * static_cast<int64_t>(p.rec), exp_off) : 0;
+                    tc_load_wait(v);
 #pragma unroll
-                            for (int i = 0; i < 4; i++) {
-                                const int4 x = eb[i];
-                                const int xs[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-                                for (int j = 0; j < 4; j++)
-                                    v[4 * i + j] = plain ? v[4 * i + j] * fa * mx_pow2(xs[j]) : ldexpf(v[4 * i + j], e + xs[j]);
-                            }
-                        }
-                        if (straight && c + 16 <= cols) {
-                            if (r < rows) store_y16(p, (tile.lo + r) * p.N + tile.n0 + c, v);
-                        } else {
-                            __syncwarp();
-#pragma unroll
-                            for (int i = 0; i < 16; i++) turn[lane * 17 + i] = v[i];
-                            __syncwarp();
-#pragma unroll 4
-                            for (int i = 0; i < 16; i++) {           // two rows of 16 values at a time
-                                const int rr = 2 * i + (lane >> 4), cc = lane & 15;
-                                if (32 * warp + rr < rows && c + cc < cols)
-                                    store_y(p, (tile.lo + 32 * warp + rr) * p.N + tile.n0 + c + cc, turn[rr * 17 + cc]);
-                            }
-                        }
-                    }
-                } else {
-                    for (int c = 0; c < rows; c += 16) {      // lanes are rows of B: 32 consecutive values of a row of Y per warp
-                        float v[16];
-                        tc_load16(acc + c, v);
-#pragma unroll
-                        for (int i = 0; i < 16; i++) {
-                            if (c + i < rows) {
-                                const int ea = BLOCK == 16 ? mx_row_exp(a + (c + i) * static_cast<int64_t>(p.rec), 0) : 0;
-                                if (r < cols) store_y(p, (tile.lo + c + i) * p.N + tile.n0 + r, BLOCK == 16 ? ldexpf(v[i], e + ea) : v[i]);
-                            }
-                        }
+                    for (int i = 0; i < 16; i++) {
+                        const int e = BLOCK == 16 ? eb + __shfl_sync(0xffffffffu, ea, i) : 0;
+                        const float y = __uint_as_float(v[i]);
+                        if (c + i < rows && r < cols) store_y(p, (tile.lo + c + i) * p.N + tile.n0 + r, BLOCK == 16 ? scaled(y, e) : y);
                     }
                 }
                 tc_fence_before();
@@ -529,58 +475,376 @@ __global__ void __launch_bounds__(MxLayout<BLOCK, QROWS>::kThreads, MxLayout<BLO
             }
             if (!ok && lane == 0) give_up();
         }
-
         if (split == 1) break;
-        if constexpr (!kWide) {
-            // ---- one tile per cluster: every CTA lays its partial sums out in its own shared memory (the stages are idle by now:
-            // all that was loaded has been multiplied), then each adds up its share of the tokens over all CTAs, in order of rank
-            const Tile tile = walk_sum.at(p, t0);
-            if (!tile.valid) break;                    // the same for the whole cluster
-            float *const part = reinterpret_cast<float *>(base_ptr);       // [QROWS][128]
-            const int rows = static_cast<int>(min(tile.hi - tile.lo, static_cast<int64_t>(MROWS)));
-            if (warp < 4) {
-                bool ok = mbar_wait_bounded(bar(&ctrl->acc_full), done & 1) && !aborted();
-                done++;
-                ok = __all_sync(0xffffffffu, ok);
-                if (!ok && lane == 0) give_up();
-                tc_fence_after();
-                if (ok) {
-                    for (int c = 0; c < rows; c += 16) {
-                        float v[16];
-                        tc_load16(tmem + (static_cast<uint32_t>(32 * warp) << 16) + c, v);
+
+        // ---- one tile per cluster: every CTA lays its partial sums out in its own shared memory (the stages are idle by now: all
+        // that was loaded has been multiplied), then each adds up its share of the tokens over all CTAs, in order of rank
+        const Tile tile = walk_sum.at(p, t0);
+        if (!tile.valid) break;                    // the same for the whole cluster
+        float *const part = reinterpret_cast<float *>(base_ptr);       // [QROWS][128]
+        const int rows = static_cast<int>(min(tile.hi - tile.lo, static_cast<int64_t>(QROWS)));
+        const int cols = static_cast<int>(min(p.N - tile.n0, static_cast<int64_t>(kRows)));
+        const uint8_t *a = p.A + tile.lo * p.rec, *b = p.B + (tile.matrix + tile.n0) * p.rec;
+        const int n = threadIdx.x & 127;           // of the first 256 threads: a column, every other one of this CTA's tokens
+        const int eb = BLOCK == 16 && n < cols ? mx_row_exp(b + n * static_cast<int64_t>(p.rec), exp_off) : 0;
+        if (warp < 4) {
+            bool ok = mbar_wait_bounded(bar(&ctrl->acc_full), done & 1) && !aborted();
+            done++;
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok && lane == 0) give_up();
+            tc_fence_after();
+            if (ok) {
+                for (int c = 0; c < rows; c += 16) {
+                    uint32_t v[16];
+                    tc_load16(tmem + (static_cast<uint32_t>(32 * warp) << 16) + c, v);
+                    tc_load_wait(v);
 #pragma unroll
-                        for (int i = 0; i < 16; i++) part[(c + i) * 128 + 32 * warp + lane] = v[i];
+                    for (int i = 0; i < 16; i++) part[(c + i) * 128 + 32 * warp + lane] = __uint_as_float(v[i]);
+                }
+            }
+            tc_fence_before();
+        }
+        cluster_barrier();
+        bool failed = false;
+        for (int q = 0; q < split; q++) failed = failed || cluster_load(smem_u32(&ctrl->abort), q) != 0;
+        if (threadIdx.x < 256 && !failed) {
+            for (int m = rank + split * (threadIdx.x >> 7); m < rows; m += 2 * split) {
+                const int ea = BLOCK == 16 ? mx_row_exp(a + m * static_cast<int64_t>(p.rec), exp_off) : 0;
+                uint32_t v[8];
+#pragma unroll
+                for (int q = 0; q < 8; q++) v[q] = q < split ? cluster_load(smem_u32(part + 128 * m + n), q) : 0;
+                float sum = __uint_as_float(v[0]);
+#pragma unroll
+                for (int q = 1; q < 8; q++) sum += __uint_as_float(v[q]);       // + 0 behind the last
+                if (n < cols) store_y(p, (tile.lo + m) * p.N + tile.n0 + n, BLOCK == 16 ? scaled(sum, ea + eb) : sum);
+            }
+        }
+        fence_async_smem();       // the next tile's copies come after these reads
+        cluster_barrier();        // and nobody leaves while others read its memory
+        if (failed) break;
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 9) {
+        tc_fence_after();
+        tc_free<false, L::kColumns>(tmem);
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ wide
+template <int BLOCK, int QROWS>
+struct WideLayout {
+    static constexpr int kHalf = QROWS / 2;                                  // rows of B that one CTA of the pair loads
+    static constexpr int kP = kRows * 128, kQ = kHalf * 128, kStage = kP + kQ;
+    static constexpr int kStages = 4;
+    static constexpr int kQGroups = QROWS / 128;                             // groups of 128 rows of scales of B
+    static constexpr int kGroup = 64 / Scales<BLOCK>::kBytes;                // stages whose scales one copy of 64 bytes a row holds
+    static constexpr int kScale = (1 + kQGroups) * kRows * 64, kScaleBufs = 2;
+    static constexpr int kScaleAt = kStages * kStage, kTurnAt = kScaleAt + kScaleBufs * kScale;
+    static constexpr int kTurn = 4096;                                       // 32 rows of 128 bytes of Y; two for each warp
+    static constexpr int kFactorAt = kTurnAt + 4 * 2 * kTurn, kCtrlAt = kFactorAt + QROWS * 4;
+    static constexpr int kBytes = 1024 + kCtrlAt + 256;
+    static constexpr int kAccs = QROWS == 256 ? 1 : 2;                       // accumulators
+    static constexpr int kWordCols = Scales<BLOCK>::kWords * 4;              // columns of 128 rows' scales of a stage
+    static constexpr int kScaleBase = kAccs * QROWS, kScaleCols = (1 + kQGroups) * 16;
+    static constexpr int kColumns = 512;
+    static_assert(kScaleBase + kStages * kScaleCols <= kColumns && kBytes <= 227 * 1024, "tensor or shared memory");
+};
+struct WideCtrl {
+    unsigned long long full[4], scale_full[2], scale_empty[2], ready[4], empty[4], acc_full[2], acc_empty[2];
+    uint32_t tmem;
+    int abort;
+};
+
+template <int BLOCK, int QROWS>
+__global__ void __launch_bounds__(kWideThreads, 1) mx_wide_kernel(const MxProductParams p, const __grid_constant__ MxMaps maps) {
+    using L = WideLayout<BLOCK, QROWS>;
+    constexpr int kWords = Scales<BLOCK>::kWords;
+    extern __shared__ uint8_t raw[];
+    const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
+    uint8_t *const base_ptr = raw + (base - smem_u32(raw));
+    WideCtrl *ctrl = reinterpret_cast<WideCtrl *>(base_ptr + L::kCtrlAt);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rank = blockIdx.x & 1;              // of the pair; the first issues the matrix instructions
+    auto bar = [&](const unsigned long long *b) { return smem_u32(b); };
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < L::kStages; i++) {
+            mbar_init(bar(&ctrl->full[i]), 1);
+            mbar_init(bar(&ctrl->ready[i]), 8);          // four warps of either CTA
+            mbar_init(bar(&ctrl->empty[i]), 1);
+        }
+        for (int i = 0; i < 2; i++) {
+            mbar_init(bar(&ctrl->scale_full[i]), 1);
+            mbar_init(bar(&ctrl->scale_empty[i]), 8);
+            mbar_init(bar(&ctrl->acc_full[i]), 1);
+            mbar_init(bar(&ctrl->acc_empty[i]), 8);
+        }
+        ctrl->abort = 0;
+        mbar_init_fence();
+    }
+    if (warp == 12 && lane < 4 + p.y_maps) tma_prefetch(&maps.a + lane);
+    if (warp == 13) tc_alloc<true, L::kColumns>(smem_u32(&ctrl->tmem));
+    tc_fence_before();
+    __syncthreads();
+    cluster_barrier();                                   // the other CTA's barriers are there
+    tc_fence_after();
+    const uint32_t tmem = ctrl->tmem;
+    grid_dependency_wait();
+
+    const int64_t first = blockIdx.x / 2, step = gridDim.x / 2;
+    auto give_up = [&]() {
+        if (p.status) atomicOr(p.status, RAC_STATUS_TIMEOUT);
+        *reinterpret_cast<volatile int *>(&ctrl->abort) = 1;
+    };
+    auto aborted = [&]() { return *reinterpret_cast<volatile int *>(&ctrl->abort) != 0; };
+    TileWalk<2 * kRows, QROWS> walk;
+    bool ok = true;
+    int it = 0, done = 0, group = 0;       // stages, tiles and scale copies that this role has gone through
+
+    if (warp == 12) {
+        // ---- TMA
+        for (int64_t t = first; ok; t += step) {
+            const Tile tile = walk.at(p, t);
+            if (!tile.valid) break;
+            if (lane == 0) {
+                const int row_a = static_cast<int>(min(tile.lo + rank * kRows, p.M)), row_b = static_cast<int>(tile.matrix + tile.n0);
+                for (int ks = 0; ks < p.k_stages; ks++, it++) {
+                    if (ks % L::kGroup == 0) {
+                        const int sb = group & 1;
+                        ok = mbar_wait_bounded(bar(&ctrl->scale_empty[sb]), (group >> 1 & 1) ^ 1) && !aborted();
+                        if (!ok) break;
+                        const uint32_t full = bar(&ctrl->scale_full[sb]), dst = base + L::kScaleAt + sb * L::kScale;
+                        mbar_arrive_expect_tx(full, L::kScale);
+                        tma_load_2d(dst, &maps.a_scale, ks / L::kGroup * 64, row_a, full);
+#pragma unroll
+                        for (int g = 0; g < L::kQGroups; g++)
+                            tma_load_2d(dst + (1 + g) * kRows * 64, &maps.b_scale, ks / L::kGroup * 64, row_b + g * kRows, full);
+                        group++;
+                    }
+                    const int st = it % L::kStages;
+                    ok = mbar_wait_bounded(bar(&ctrl->empty[st]), (it / L::kStages & 1) ^ 1);
+                    if (!ok) break;
+                    const uint32_t full = bar(&ctrl->full[st]), dst = base + st * L::kStage;
+                    mbar_arrive_expect_tx(full, L::kStage + p.test_extra_tx);
+                    tma_load_2d(dst, &maps.a, ks * 128, row_a, full);
+                    tma_load_2d(dst + L::kP, &maps.b, ks * 128, row_b + rank * L::kHalf, full);
+                }
+                if (!ok) give_up();
+            }
+            ok = __shfl_sync(0xffffffffu, ok, 0);
+        }
+        if (!ok && lane == 0) {      // copies in flight must land before the CTA's memory is given back
+            for (int i = max(0, it - L::kStages); i < it; i++) mbar_wait_bounded(bar(&ctrl->full[i % L::kStages]), i / L::kStages & 1);
+            for (int i = max(0, group - 2); i < group; i++) mbar_wait_bounded(bar(&ctrl->scale_full[i & 1]), i >> 1 & 1);
+        }
+    } else if (warp == 13) {
+        // ---- matrix instructions, for both CTAs
+        for (int64_t t = first; ok && rank == 0; t += step, done++) {
+            const Tile tile = walk.at(p, t);
+            if (!tile.valid) break;
+            if (lane == 0) {
+                const int ab = done % L::kAccs;
+                const uint32_t acc = tmem + ab * QROWS;
+                ok = mbar_wait_bounded(bar(&ctrl->acc_empty[ab]), (done / L::kAccs & 1) ^ 1) && !aborted();
+                tc_fence_after();
+                for (int ks = 0; ok && ks < p.k_stages; ks++, it++) {
+                    const int st = it % L::kStages;
+                    ok = mbar_wait_bounded(bar(&ctrl->ready[st]), it / L::kStages & 1);
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint32_t sp = tmem + L::kScaleBase + st * L::kScaleCols, sq = sp + 16;
+                    const uint64_t dp = desc_codes(base + st * L::kStage), dq = desc_codes(base + st * L::kStage + L::kP);
+                    tc_stage<BLOCK, true, QROWS, 4 * L::kQGroups>(min(4, (p.d - ks * kStageK + 63) / 64), acc, dp, dq, sp, sq, ks > 0);
+                    tc_commit<true>(bar(&ctrl->empty[st]));
+                }
+                if (!ok) give_up();
+                tc_commit<true>(bar(&ctrl->acc_full[ab]));
+                // what was issued ends before its operands and sums are given back
+                if (!ok) mbar_wait_bounded(bar(&ctrl->acc_full[ab]), done / L::kAccs & 1);
+            }
+            ok = __shfl_sync(0xffffffffu, ok, 0);
+        }
+    } else if (warp >= 4) {
+        // ---- scales, a quarter of the lanes each; two teams of four warps take turns, a stage each
+        const uint32_t quarter = static_cast<uint32_t>(32 * (warp & 3)) << 16;
+        const int team = (warp - 4) >> 2;
+        const int turn = lane >> 1 & 3;              // 64-byte swizzle: 16-byte piece c of row r lies at c ^ (r / 2 mod 4)
+        for (int64_t t = first; ok; t += step) {
+            const Tile tile = walk.at(p, t);
+            if (!tile.valid) break;
+            for (int ks = 0; ks < p.k_stages; ks++, it++) {
+                const int st = it % L::kStages, sub = ks % L::kGroup, sb = group & 1;
+                const bool last = sub == L::kGroup - 1 || ks == p.k_stages - 1;
+                group += last;
+                if ((it & 1) != team) {
+                    if (last && lane == 0) mbar_arrive(bar(&ctrl->scale_empty[sb]));
+                    continue;
+                }
+                ok = mbar_wait_bounded(bar(&ctrl->scale_full[sb]), (group - last) >> 1 & 1) && mbar_wait_bounded(bar(&ctrl->full[st]), it / L::kStages & 1);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t at = base + L::kScaleAt + sb * L::kScale + lane * 64 +
+                                    (BLOCK == 16 ? (sub ^ turn) * 16 : (sub / 2 ^ turn) * 16 + 8 * (sub & 1));
+                const int left = p.nblk - ks * Scales<BLOCK>::kBytes;
+                const uint32_t to = tmem + quarter + L::kScaleBase + st * L::kScaleCols;
+                uint32_t w[1 + L::kQGroups][kWords * 4];
+#pragma unroll
+                for (int g = 0; g < 1 + L::kQGroups; g++) load_scales<BLOCK, 4>(w[g], at + g * kRows * 64, 32 * 64, left);
+                tc_store<kWords * 4>(to, w[0]);
+                if constexpr (L::kQGroups == 1) {
+                    tc_store<kWords * 4>(to + 16, w[1]);
+                } else {      // the eight groups of 32 rows beside one another
+                    uint32_t q[kWords * 8];
+#pragma unroll
+                    for (int j = 0; j < kWords; j++)
+#pragma unroll
+                        for (int g = 0; g < 8; g++) q[8 * j + g] = w[1 + g / 4][4 * j + g % 4];
+#pragma unroll
+                    for (int j = 0; j < kWords / 2; j++) tc_store<16>(to + 16 + 16 * j, q + 16 * j);
+                }
+                tc_store_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    mbar_arrive_at(bar(&ctrl->ready[st]), 0);
+                    if (last) mbar_arrive(bar(&ctrl->scale_empty[sb]));
+                }
+            }
+        }
+        if (!ok && lane == 0) give_up();
+    } else {
+        // ---- epilogue: 32 lanes of the accumulator each, 128 bytes of a row of Y at a time, through shared memory
+        float *const factor = reinterpret_cast<float *>(base_ptr + L::kFactorAt);
+        const uint32_t turn0 = base + L::kTurnAt + warp * 2 * L::kTurn;
+        const int exp_off = p.scale_off + p.nblk;
+        const int r = 32 * warp + lane;            // this thread's lane of the accumulator
+        const bool wide_y = p.y_type == RAC_MX_FP32;
+        const int per = wide_y ? 32 : 64;          // values of a row of Y per turn
+        int turns = 0;
+        for (int64_t t = first; ok; t += step, done++) {
+            const Tile tile = walk.at(p, t);
+            if (!tile.valid) break;
+            const int64_t row0 = tile.lo + rank * kRows;
+            const int rows = static_cast<int>(max(static_cast<int64_t>(0), min(tile.hi - row0, static_cast<int64_t>(kRows))));
+            const int cols = static_cast<int>(min(p.N - tile.n0, static_cast<int64_t>(QROWS)));
+            const int ab = done % L::kAccs;
+            const uint32_t acc = tmem + ab * QROWS + (static_cast<uint32_t>(32 * warp) << 16);
+            int e = 0;
+            bool plain = true;                     // exponents so small that their factors multiply without loss
+            if (BLOCK == 16) {
+                const uint8_t *a = p.A + row0 * p.rec, *b = p.B + (tile.matrix + tile.n0) * p.rec;
+                asm volatile("bar.sync 1, 128;" ::: "memory");           // the tile before has read its factors
+                e = r < rows ? mx_row_exp(a + r * static_cast<int64_t>(p.rec), exp_off) : 0;
+                plain = e >= -50 && e <= 50;
+                for (int c = r; c < QROWS; c += 128) {
+                    const int eb = c < cols ? mx_row_exp(b + c * static_cast<int64_t>(p.rec), exp_off) : 0;
+                    factor[c] = __int_as_float(eb);
+                    plain = plain && eb >= -50 && eb <= 50;
+                }
+                uint32_t all;
+                asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbar.red.and.pred q, 1, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                             : "=r"(all) : "r"(static_cast<uint32_t>(plain)) : "memory");
+                plain = all != 0;
+                if (plain) {
+                    for (int c = r; c < QROWS; c += 128) factor[c] = mx_pow2(__float_as_int(factor[c]));
+                    asm volatile("bar.sync 1, 128;" ::: "memory");
+                }
+            }
+            ok = mbar_wait_bounded(bar(&ctrl->acc_full[ab]), done / L::kAccs & 1) && !aborted();
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            tc_fence_after();
+            const float fa = plain ? mx_pow2(e) : 0.0f;
+            const int mine = min(32, rows - 32 * warp);                  // rows of this warp
+            for (int c0 = 0; c0 < cols && mine > 0; c0 += per, turns++) {
+                const uint32_t turn = turn0 + (turns & 1) * L::kTurn;
+                if (lane == 0) bulk_wait_read<1>();                      // the store before the last has left this buffer
+                __syncwarp();
+#pragma unroll 1
+                for (int c = 0; c < per; c += 32) {
+                    uint32_t v[2][16];
+                    tc_load16(acc + c0 + c, v[0]);
+                    tc_load16(acc + c0 + c + 16, v[1]);
+                    tc_load_wait(v[0]);
+                    tc_load_wait(v[1]);
+#pragma unroll
+                    for (int h = 0; h < 2; h++) {
+                        float y[16];
+#pragma unroll
+                        for (int i = 0; i < 16; i++) y[i] = __uint_as_float(v[h][i]);
+                        if (BLOCK == 16) {
+                            const float4 *f = reinterpret_cast<const float4 *>(factor + c0 + c + 16 * h);
+                            if (plain) {
+#pragma unroll
+                                for (int i = 0; i < 4; i++) {
+                                    const float4 x = f[i];
+                                    y[4 * i] *= fa * x.x;
+                                    y[4 * i + 1] *= fa * x.y;
+                                    y[4 * i + 2] *= fa * x.z;
+                                    y[4 * i + 3] *= fa * x.w;
+                                }
+                            } else {
+#pragma unroll
+                                for (int i = 0; i < 16; i++) y[i] = ldexpf(y[i], e + __float_as_int(factor[c0 + c + 16 * h + i]));
+                            }
+                        }
+                        // piece q (16 bytes) of a row lies at q ^ (row mod 8): the 128-byte swizzle of the copy
+                        if (wide_y) {
+#pragma unroll
+                            for (int i = 0; i < 4; i++)
+                                sts128(turn + lane * 128 + ((4 * h + i) ^ (lane & 7)) * 16,
+                                       make_uint4(__float_as_uint(y[4 * i]), __float_as_uint(y[4 * i + 1]), __float_as_uint(y[4 * i + 2]), __float_as_uint(y[4 * i + 3])));
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < 2; i++)
+                                sts128(turn + lane * 128 + ((c / 8 + 2 * h + i) ^ (lane & 7)) * 16,
+                                       make_uint4(pack16(p.y_type, y[8 * i], y[8 * i + 1]), pack16(p.y_type, y[8 * i + 2], y[8 * i + 3]),
+                                                  pack16(p.y_type, y[8 * i + 4], y[8 * i + 5]), pack16(p.y_type, y[8 * i + 6], y[8 * i + 7])));
+                        }
                     }
                 }
-                tc_fence_before();
-            }
-            cluster_barrier();
-            bool failed = false;
-            for (int q = 0; q < split; q++) failed = failed || cluster_load(smem_u32(&ctrl->abort), q) != 0;
-            const int exp_off = p.scale_off + p.nblk;
-            const uint8_t *a = p.A + tile.lo * p.rec + exp_off, *b = p.B + (tile.matrix + tile.n0) * p.rec + exp_off;
-            const int cols = static_cast<int>(min(p.N - tile.n0, static_cast<int64_t>(NROWS)));
-            const int share = (rows * 128 + split - 1) / split;
-            for (int i = rank * share + threadIdx.x; !failed && i < min(rows * 128, (rank + 1) * share); i += blockDim.x) {
-                const int m = i >> 7, n = i & 127;
-                float sum = 0.0f;
-                for (int q = 0; q < split; q++) sum += __uint_as_float(cluster_load(smem_u32(part) + 4 * i, q));
-                if (n < cols) {
-                    int e = 0;
-                    if (BLOCK == 16)
-                        e = mx_row_exp(a + m * static_cast<int64_t>(p.rec), 0) + mx_row_exp(b + n * static_cast<int64_t>(p.rec), 0);
-                    store_y(p, (tile.lo + m) * p.N + tile.n0 + n, BLOCK == 16 ? ldexpf(sum, e) : sum);
+                if (p.y_maps && mine == 32) {
+                    fence_async_smem();
+                    __syncwarp();
+                    if (lane == 0) {
+                        tma_store_2d(&maps.y, static_cast<int>(tile.n0) + c0, static_cast<int>(row0) + 32 * warp, turn);
+                        bulk_commit();
+                    }
+                } else {
+                    // rows that are not all this segment's, or that start where TMA cannot: a row at a time
+                    __syncwarp();
+                    for (int i = 0; i < mine; i++) {
+                        const int64_t at = (row0 + 32 * warp + i) * p.N + tile.n0 + c0;
+                        for (int c = lane; c < min(per, cols - c0); c += 32) {
+                            const int piece = c * (wide_y ? 4 : 2);
+                            const uint32_t src = turn + i * 128 + ((piece >> 4) ^ (i & 7)) * 16 + (piece & 15);
+                            if (wide_y) {
+                                static_cast<uint32_t *>(p.Y)[at + c] = lds32(src);
+                            } else {
+                                uint16_t v;
+                                asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(src));
+                                static_cast<uint16_t *>(p.Y)[at + c] = v;
+                            }
+                        }
+                    }
+                    __syncwarp();
                 }
             }
-            fence_async_smem();       // the next tile's copies come after these reads
-            cluster_barrier();        // and nobody leaves while others read its memory
-            if (failed) break;
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_at(bar(&ctrl->acc_empty[ab]), 0);
         }
+        if (lane == 0) bulk_wait_all();
+        if (!ok && lane == 0) give_up();
     }
+    tc_fence_before();
     __syncthreads();
-    if (warp == 5) {
+    cluster_barrier();        // nobody leaves while the other's instructions read its memory or arrive at its barriers
+    if (warp == 13) {
         tc_fence_after();
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(L::kColumns) : "memory");
+        tc_free<true, L::kColumns>(tmem);
     }
 }
 
@@ -597,16 +861,24 @@ static EncodeTiled encode_tiled() {
     }();
     return fn;
 }
-// The codes of `rows` records as a matrix of bytes, in boxes of 128 bytes by `box` rows; bytes beyond the codes and rows beyond
-// the last read as zero.  Every box starts at a multiple of 128 bytes.
-static bool codes_map(CUtensorMap *map, const uint8_t *recs, int64_t rows, const MxProductParams &p, int box) {
+static bool tensor_map(CUtensorMap *map, CUtensorMapDataType type, const void *at, int64_t width, int64_t rows, int64_t stride, int box_w, int box_h,
+                       CUtensorMapSwizzle swizzle) {
     const EncodeTiled fn = encode_tiled();
     if (!fn) return false;
-    const cuuint64_t dims[2] = {static_cast<cuuint64_t>(p.d / 2), static_cast<cuuint64_t>(rows)};
-    const cuuint64_t strides[1] = {static_cast<cuuint64_t>(p.rec)};
-    const cuuint32_t boxes[2] = {128, static_cast<cuuint32_t>(box)}, one[2] = {1, 1};
-    return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<uint8_t *>(recs), dims, strides, boxes, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
-              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    const cuuint64_t dims[2] = {static_cast<cuuint64_t>(width), static_cast<cuuint64_t>(rows)};
+    const cuuint64_t strides[1] = {static_cast<cuuint64_t>(stride)};
+    const cuuint32_t boxes[2] = {static_cast<cuuint32_t>(box_w), static_cast<cuuint32_t>(box_h)}, one[2] = {1, 1};
+    return fn(map, type, 2, const_cast<void *>(at), dims, strides, boxes, one, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
+              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+// The codes of records as a matrix of bytes, in boxes of 128 bytes by `box` rows, and their scales (with what lies behind them up
+// to the next multiple of 16 bytes), in boxes of `width` bytes.  What lies outside reads as zero; every box starts at a
+// multiple of its width.
+static bool record_maps(CUtensorMap *codes, CUtensorMap *scales, const uint8_t *recs, int64_t rows, const MxProductParams &p, int box, int scale_width,
+                        int scale_box) {
+    return tensor_map(codes, CU_TENSOR_MAP_DATA_TYPE_UINT8, recs, p.d / 2, rows, p.rec, 128, box, CU_TENSOR_MAP_SWIZZLE_128B) &&
+           tensor_map(scales, CU_TENSOR_MAP_DATA_TYPE_UINT8, recs + p.scale_off, (p.nblk + 15) / 16 * 16, rows, p.rec, scale_width, scale_box,
+                      scale_width == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_NONE);
 }
 
 static int sm_count() {
@@ -614,40 +886,62 @@ static int sm_count() {
     if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
     return n;
 }
+// Tiles of `rows` rows of A, at most: with segments the lengths are on the device, and each may end in a tile that is not full.
+static int64_t row_tiles(const MxProductParams &p, int rows) {
+    if (!p.seg_off) return (p.M + rows - 1) / rows;
+    return p.M < p.n_seg ? p.M : (p.M - p.n_seg) / rows + p.n_seg;
+}
+static int64_t weight_rows(const MxProductParams &p) { return p.seg_off ? p.n_seg * p.N : p.N; }
 
 template <int BLOCK, int QROWS>
-static int launch_mx_product(MxProductParams p, cudaStream_t s) {
-    using L = MxLayout<BLOCK, QROWS>;
-    constexpr int MROWS = L::kWide ? kPRows : QROWS, NROWS = L::kWide ? QROWS : kPRows;
-    const int sms = sm_count();
-    if (sms <= 0) return RAC_ECUDA;
-    CUtensorMap map_a, map_b;
-    if (!codes_map(&map_a, p.A, p.M, p, MROWS) || !codes_map(&map_b, p.B, p.seg_off ? p.n_seg * p.N : p.N, p, NROWS)) return RAC_ECUDA;
-    p.n_tiles = static_cast<int>((p.N + NROWS - 1) / NROWS);
-    // with segments the lengths are on the device: each may end in a tile that is not full
-    int64_t tiles = (p.M + MROWS - 1) / MROWS;
-    if (p.seg_off) tiles = p.M < p.n_seg ? p.M : (p.M - p.n_seg) / MROWS + p.n_seg;
-    tiles *= p.n_tiles;
-    const int64_t slots = L::kWide ? sms : 2 * sms;
+static int launch_narrow(MxProductParams p, int sms, cudaStream_t s) {
+    using L = NarrowLayout<QROWS>;
+    MxMaps maps = {};
+    if (!record_maps(&maps.a, &maps.a_scale, p.A, p.M, p, QROWS, 16, QROWS) ||
+        !record_maps(&maps.b, &maps.b_scale, p.B, weight_rows(p), p, kRows, 16, kRows))
+        return RAC_ECUDA;
+    p.n_tiles = static_cast<int>((p.N + kRows - 1) / kRows);
+    const int64_t tiles = row_tiles(p, QROWS) * p.n_tiles, slots = 2 * sms;
     p.split = 1;
-    if (!L::kWide)
-        while (p.split < 8 && tiles * p.split * 2 <= slots && p.split * 2 <= p.k_stages) p.split *= 2;
+    while (p.split < 8 && tiles * p.split * 2 <= slots && p.split * 2 <= p.k_stages) p.split *= 2;
     const int64_t ctas = p.split > 1 ? tiles * p.split : (tiles < slots ? tiles : slots);
-    auto kernel = mx_product_kernel<BLOCK, QROWS>;
+    auto kernel = mx_narrow_kernel<BLOCK, QROWS>;
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kBytes) != cudaSuccess) return RAC_ECUDA;
-    if (p.split > 1) launch_cluster_after(kernel, static_cast<unsigned>(ctas), p.split, L::kThreads, L::kBytes, s, p, map_a, map_b);
-    else launch_after(kernel, static_cast<unsigned>(ctas), L::kThreads, L::kBytes, s, p, map_a, map_b);
+    if (p.split > 1) launch_cluster_after(kernel, static_cast<unsigned>(ctas), p.split, kNarrowThreads, L::kBytes, s, p, maps);
+    else launch_after(kernel, static_cast<unsigned>(ctas), kNarrowThreads, L::kBytes, s, p, maps);
+    return cudaGetLastError() == cudaSuccess ? RAC_OK : RAC_ECUDA;
+}
+
+template <int BLOCK, int QROWS>
+static int launch_wide(MxProductParams p, int sms, cudaStream_t s) {
+    using L = WideLayout<BLOCK, QROWS>;
+    MxMaps maps = {};
+    if (!record_maps(&maps.a, &maps.a_scale, p.A, p.M, p, kRows, 64, kRows) ||
+        !record_maps(&maps.b, &maps.b_scale, p.B, weight_rows(p), p, L::kHalf, 64, kRows))
+        return RAC_ECUDA;
+    const int esize = p.y_type == RAC_MX_FP32 ? 4 : 2;
+    p.y_maps = p.N * esize % 16 == 0;
+    if (p.y_maps && !tensor_map(&maps.y, p.y_type == RAC_MX_FP32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_UINT16, p.Y, p.N, p.M,
+                                p.N * esize, 128 / esize, 32, CU_TENSOR_MAP_SWIZZLE_128B))
+        return RAC_ECUDA;
+    p.n_tiles = static_cast<int>((p.N + QROWS - 1) / QROWS);
+    const int64_t tiles = row_tiles(p, 2 * kRows) * p.n_tiles, pairs = sms / 2;
+    auto kernel = mx_wide_kernel<BLOCK, QROWS>;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kBytes) != cudaSuccess) return RAC_ECUDA;
+    launch_cluster_after(kernel, static_cast<unsigned>(2 * (tiles < pairs ? tiles : pairs)), 2, kWideThreads, L::kBytes, s, p, maps);
     return cudaGetLastError() == cudaSuccess ? RAC_OK : RAC_ECUDA;
 }
 
 template <int BLOCK>
 static int dispatch_mx_product(const MxProductParams &p, cudaStream_t s) {
+    const int sms = sm_count();
+    if (sms <= 0) return RAC_ECUDA;
     // rows per weight matrix, on average
     const int64_t rows = (p.M + p.n_seg - 1) / p.n_seg;
-    if (rows > 128) return launch_mx_product<BLOCK, 256>(p, s);
-    if (rows > 64) return launch_mx_product<BLOCK, 128>(p, s);
-    if (rows > 16) return launch_mx_product<BLOCK, 64>(p, s);
-    return launch_mx_product<BLOCK, 16>(p, s);
+    if (rows > 128) return launch_wide<BLOCK, 256>(p, sms, s);
+    if (rows > 64) return launch_narrow<BLOCK, 128>(p, sms, s);
+    if (rows > 16) return launch_narrow<BLOCK, 64>(p, sms, s);
+    return launch_narrow<BLOCK, 16>(p, sms, s);
 }
 
 static int mx_product_impl(const rac_mx_cfg *cfg, const void *A, int64_t M, const int32_t *seg_off, int64_t n_seg, const void *B,
