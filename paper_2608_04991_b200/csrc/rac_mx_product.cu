@@ -17,7 +17,7 @@
 //           fill the 128 lanes and a handful of tokens costs a handful of columns.  What bounds it is reading the weights;
 //           where the tiles alone do not fill the SMs, clusters split the channels and add their partial sums through
 //           distributed shared memory in a fixed order.
-// Warps 0-3 of a CTA are the epilogue, 4-7 (wide: 4-11) carry scales, the next issues TMA loads and the last the matrix
+// Warps 0-3 of a CTA are the epilogue, 4-11 carry scales, the next issues TMA loads and the last the matrix
 // instructions.  Every wait on an mbarrier is bounded: a copy that never lands ends the kernel with RAC_STATUS_TIMEOUT.
 #include <cuda.h>
 
@@ -27,7 +27,7 @@ namespace rac {
 
 constexpr int kStageK = 256;             // channels per pipeline stage: one 128-byte row of codes
 constexpr int kRows = 128;               // lanes of an accumulator
-constexpr int kNarrowThreads = 320, kWideThreads = 448;
+constexpr int kThreads = 448;
 
 struct MxProductParams {
     const uint8_t *A, *B;
@@ -41,6 +41,7 @@ struct MxProductParams {
     int n_tiles;              // tiles along N
     int split;                // narrow: CTAs of a cluster that share the channels of a tile, 1 = none
     int y_maps;               // wide: Y has rows that TMA can store
+    int early;                // the next kernel on the stream may be set up from the start
     uint32_t test_extra_tx;   // rac_mx_selftest_bounded_wait: bytes announced beyond what a stage's copies deliver
 };
 struct MxMaps {
@@ -72,16 +73,19 @@ __device__ __forceinline__ void mbar_arrive_at(uint32_t bar, uint32_t rank) {
                  "mbarrier.arrive.shared::cluster.b64 _, [far];\n\t}" ::"r"(bar), "r"(rank)
                  : "memory");
 }
-// all threads of the cluster
-__device__ __forceinline__ void cluster_barrier() {
-    asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
+// all threads of the cluster, nothing ordered by it
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait;" ::: "memory"); }
+// a place in the shared memory of the cluster's CTA `rank`
+__device__ __forceinline__ uint32_t cluster_at(uint32_t addr, uint32_t rank) {
+    uint32_t far;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(far) : "r"(addr), "r"(rank));
+    return far;
 }
-// a word of the shared memory of the cluster's CTA `rank`, at the place `addr` has in this one's
-__device__ __forceinline__ uint32_t cluster_load(uint32_t addr, uint32_t rank) {
-    uint32_t v;
-    asm volatile("{\n\t.reg .b32 far;\n\tmapa.shared::cluster.u32 far, %1, %2;\n\tld.shared::cluster.u32 %0, [far];\n\t}"
-                 : "=r"(v) : "r"(addr), "r"(rank));
-    return v;
+// copies `bytes` from this CTA's shared memory there, counted on that CTA's mbarrier
+__device__ __forceinline__ void cluster_push(uint32_t far, uint32_t src, uint32_t bytes, uint32_t far_bar) {
+    asm volatile("cp.async.bulk.shared::cluster.shared::cta.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 ::"r"(far), "r"(src), "r"(bytes), "r"(far_bar) : "memory");
 }
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -194,7 +198,7 @@ struct TileWalk {
     int s = 0;
     __device__ __forceinline__ Tile at(const MxProductParams &p, int64_t t) {
         Tile r;
-        const int64_t mt = t / p.n_tiles;
+        const int64_t mt = t <= INT32_MAX ? static_cast<int32_t>(t) / p.n_tiles : t / p.n_tiles;
         r.n0 = (t - mt * p.n_tiles) * NROWS;
         if (!p.seg_off) {
             r.lo = mt * MROWS;
@@ -293,27 +297,32 @@ struct NarrowLayout {
     static constexpr int kP = kRows * 128, kQ = QROWS * 128, kPScale = kRows * 16, kQScale = QROWS * 16;   // bytes
     static constexpr int kTx = kP + kQ + kPScale + kQScale;
     static constexpr int kStage = (kTx + 1023) / 1024 * 1024;
-    static constexpr int kStages = QROWS == 128 ? 3 : QROWS == 64 ? 4 : 5;
-    static constexpr int kBytes = 1024 + kStages * kStage + 256;             // 1024: alignment of the tiles
+    static constexpr int kStages = QROWS == 64 ? 3 : 4;
+    // split: what the other CTAs of the cluster push, [rank][token][128] (this CTA's own sums lie in the idle stages)
+    static constexpr int kPart = (QROWS == 64 ? 60 : 18) * 512;              // the most that (s - 1) * ceil(QROWS / s) is, up to 8
+    static constexpr int kPartAt = kStages * kStage, kCtrlAt = kPartAt + kPart;
+    static constexpr int kBytes = 1024 + kCtrlAt + 256;                      // 1024: alignment of the tiles
+    static constexpr int kMaxSplit = 8;
+    static constexpr int part(int s) { return (s - 1) * ((QROWS + s - 1) / s) * 512; }
     static constexpr int kGroups = QROWS > 32 ? QROWS / 32 : 1;              // groups of 32 rows of Q
-    static constexpr int kColumns = 256, kScaleBase = QROWS == 128 ? 128 : 64, kScaleCols = 32;
+    static constexpr int kColumns = 256, kScaleBase = 64, kScaleCols = 32;
     static_assert(kScaleBase + kStages * kScaleCols <= kColumns, "tensor memory");
     static_assert(kBytes > 77 * 1024 && kBytes <= 113 * 1024, "two CTAs an SM and no third, whose columns would not fit");
 };
 struct NarrowCtrl {
-    unsigned long long full[5], ready[5], empty[5], acc_full, acc_empty;
+    unsigned long long full[4], ready[4], empty[4], acc_full, acc_empty, parts;
     uint32_t tmem;
     int abort;
 };
 
 template <int BLOCK, int QROWS>
-__global__ void __launch_bounds__(kNarrowThreads, 2) mx_narrow_kernel(const MxProductParams p, const __grid_constant__ MxMaps maps) {
+__global__ void __launch_bounds__(kThreads, 2) mx_narrow_kernel(const MxProductParams p, const __grid_constant__ MxMaps maps) {
     using L = NarrowLayout<QROWS>;
     constexpr int kWords = Scales<BLOCK>::kWords;
     extern __shared__ uint8_t raw[];
     const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
     uint8_t *const base_ptr = raw + (base - smem_u32(raw));
-    NarrowCtrl *ctrl = reinterpret_cast<NarrowCtrl *>(base_ptr + L::kStages * L::kStage);
+    NarrowCtrl *ctrl = reinterpret_cast<NarrowCtrl *>(base_ptr + L::kCtrlAt);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     auto bar = [&](const unsigned long long *b) { return smem_u32(b); };
 
@@ -325,17 +334,18 @@ __global__ void __launch_bounds__(kNarrowThreads, 2) mx_narrow_kernel(const MxPr
         }
         mbar_init(bar(&ctrl->acc_full), 1);
         mbar_init(bar(&ctrl->acc_empty), 4);
+        mbar_init(bar(&ctrl->parts), 1);
         ctrl->abort = 0;
         mbar_init_fence();
     }
-    if (warp == 8 && lane < 4) tma_prefetch(&maps.a + lane);
-    if (warp == 9) tc_alloc<false, L::kColumns>(smem_u32(&ctrl->tmem));
+    if (p.early) grid_launch_dependents();
+    if (warp == 12 && lane < 4) tma_prefetch(&maps.a + lane);
+    if (warp == 13) tc_alloc<false, L::kColumns>(smem_u32(&ctrl->tmem));
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = ctrl->tmem;
-    grid_dependency_wait();
-
+    if (p.split > 1) cluster_arrive();         // this CTA's barriers are there
     // this CTA's tiles, and its share of the channels of each
     const int split = p.split;
     const int rank = split > 1 ? static_cast<int>(blockIdx.x % split) : 0;
@@ -347,22 +357,27 @@ __global__ void __launch_bounds__(kNarrowThreads, 2) mx_narrow_kernel(const MxPr
     };
     auto aborted = [&]() { return *reinterpret_cast<volatile int *>(&ctrl->abort) != 0; };
     TileWalk<QROWS, kRows> walk, walk_sum;
+    Tile head;                  // the first tile, worked out before the wait where it takes no memory to know it
+    if (!p.seg_off) head = walk.at(p, first);
+    grid_dependency_wait();
+    if (p.seg_off) head = walk.at(p, first);
     int it = 0, done = 0;       // stages and tiles that this role has gone through
+    bool pushed = false;
     const int exp_off = p.scale_off + p.nblk;
 
     // Without split one pass of this loop, in which every role goes through all of the CTA's tiles; with split one per tile.
     for (int64_t t0 = first;; t0 += step) {
-        if (warp == 8) {
+        if (warp == 12) {
             // ---- TMA
             bool ok = true;
             for (int64_t t = t0; ok; t += step) {
-                const Tile tile = walk.at(p, t);
+                const Tile tile = t == first ? head : walk.at(p, t);
                 if (!tile.valid) break;
                 if (lane == 0) {
                     const int row_a = static_cast<int>(tile.lo), row_b = static_cast<int>(tile.matrix + tile.n0);
                     for (int ks = ks0; ks < ks1; ks++, it++) {
                         const int st = it % L::kStages;
-                        if (!mbar_wait_bounded(bar(&ctrl->empty[st]), (it / L::kStages & 1) ^ 1) || aborted()) {
+                        if (!mbar_wait_bounded(bar(&ctrl->empty[st]), (it / L::kStages & 1) ^ 1)) {
                             give_up();
                             ok = false;
                             break;
@@ -382,11 +397,11 @@ __global__ void __launch_bounds__(kNarrowThreads, 2) mx_narrow_kernel(const MxPr
             if (!ok && lane == 0) {      // copies in flight must land before the CTA's memory is given back
                 for (int i = max(0, it - L::kStages); i < it; i++) mbar_wait_bounded(bar(&ctrl->full[i % L::kStages]), i / L::kStages & 1);
             }
-        } else if (warp == 9) {
+        } else if (warp == 13) {
             // ---- matrix instructions
             bool ok = true;
             for (int64_t t = t0; ok; t += step) {
-                const Tile tile = walk.at(p, t);
+                const Tile tile = t == first ? head : walk.at(p, t);
                 if (!tile.valid) break;
                 if (lane == 0) {
                     ok = split > 1 || mbar_wait_bounded(bar(&ctrl->acc_empty), (done & 1) ^ 1);
@@ -394,7 +409,7 @@ __global__ void __launch_bounds__(kNarrowThreads, 2) mx_narrow_kernel(const MxPr
                     for (int ks = ks0; ok && ks < ks1; ks++, it++) {
                         const int st = it % L::kStages;
                         const uint32_t phase = it / L::kStages & 1;
-                        ok = mbar_wait_bounded(bar(&ctrl->full[st]), phase) && mbar_wait_bounded(bar(&ctrl->ready[st]), phase) && !aborted();
+                        ok = mbar_wait_bounded(bar(&ctrl->full[st]), phase) && mbar_wait_bounded(bar(&ctrl->ready[st]), phase);
                         if (!ok) break;
                         tc_fence_after();
                         const uint32_t sp = tmem + L::kScaleBase + st * L::kScaleCols, sq = sp + 16;
@@ -412,17 +427,20 @@ __global__ void __launch_bounds__(kNarrowThreads, 2) mx_narrow_kernel(const MxPr
                 if (split > 1) break;
             }
         } else if (warp >= 4) {
-            // ---- scales, a quarter of the lanes each
-            const uint32_t quarter = static_cast<uint32_t>(32 * (warp - 4)) << 16;
+            // ---- scales, a quarter of the lanes each; two teams of four warps take turns, a stage each
+            const uint32_t quarter = static_cast<uint32_t>(32 * (warp & 3)) << 16;
+            const int team = (warp - 4) >> 2;
             bool ok = true;
             for (int64_t t = t0; ok; t += step) {
-                const Tile tile = walk.at(p, t);
+                const Tile tile = t == first ? head : walk.at(p, t);
                 if (!tile.valid) break;
                 for (int ks = ks0; ks < ks1; ks++, it++) {
+                    // both teams wait for every stage: a team that left one out could take its phase for the next but one
                     const int st = it % L::kStages;
-                    ok = mbar_wait_bounded(bar(&ctrl->full[st]), it / L::kStages & 1) && !aborted();
+                    ok = mbar_wait_bounded(bar(&ctrl->full[st]), it / L::kStages & 1);
                     ok = __all_sync(0xffffffffu, ok);
                     if (!ok) break;
+                    if ((it & 1) != team) continue;
                     tc_fence_after();
                     const uint32_t at = base + st * L::kStage + L::kP + L::kQ + (BLOCK == 32 ? 8 * (ks & 1) : 0);
                     const int left = p.nblk - ks * Scales<BLOCK>::kBytes;
@@ -445,8 +463,9 @@ __global__ void __launch_bounds__(kNarrowThreads, 2) mx_narrow_kernel(const MxPr
             const uint32_t acc = tmem + (static_cast<uint32_t>(32 * warp) << 16);
             const int r = 32 * warp + lane;
             bool ok = true;
+
             for (int64_t t = t0; ok; t += step, done++) {
-                const Tile tile = walk.at(p, t);
+                const Tile tile = t == first ? head : walk.at(p, t);
                 if (!tile.valid) break;
                 const int rows = static_cast<int>(min(tile.hi - tile.lo, static_cast<int64_t>(QROWS)));
                 const int cols = static_cast<int>(min(p.N - tile.n0, static_cast<int64_t>(kRows)));
@@ -477,21 +496,23 @@ __global__ void __launch_bounds__(kNarrowThreads, 2) mx_narrow_kernel(const MxPr
         }
         if (split == 1) break;
 
-        // ---- one tile per cluster: every CTA lays its partial sums out in its own shared memory (the stages are idle by now: all
-        // that was loaded has been multiplied), then each adds up its share of the tokens over all CTAs, in order of rank
+        // ---- one tile per cluster: every CTA lays its partial sums out in its own shared memory, copies to each other CTA those
+        // of the tokens that are that one's, and adds up its own tokens in order of rank
         const Tile tile = walk_sum.at(p, t0);
         if (!tile.valid) break;                    // the same for the whole cluster
-        float *const part = reinterpret_cast<float *>(base_ptr);       // [QROWS][128]
+        const bool more = walk_sum.at(p, t0 + step).valid;             // only where segments overlap
         const int rows = static_cast<int>(min(tile.hi - tile.lo, static_cast<int64_t>(QROWS)));
         const int cols = static_cast<int>(min(p.N - tile.n0, static_cast<int64_t>(kRows)));
-        const uint8_t *a = p.A + tile.lo * p.rec, *b = p.B + (tile.matrix + tile.n0) * p.rec;
-        const int n = threadIdx.x & 127;           // of the first 256 threads: a column, every other one of this CTA's tokens
-        const int eb = BLOCK == 16 && n < cols ? mx_row_exp(b + n * static_cast<int64_t>(p.rec), exp_off) : 0;
+        const int each = (rows + split - 1) / split, mine = max(0, min(each, rows - rank * each));     // tokens per CTA, and here
         if (warp < 4) {
-            bool ok = mbar_wait_bounded(bar(&ctrl->acc_full), done & 1) && !aborted();
-            done++;
-            ok = __all_sync(0xffffffffu, ok);
-            if (!ok && lane == 0) give_up();
+            const int n = 32 * warp + lane;        // row of B: this thread's lane of the accumulator
+            const uint8_t *a = p.A + (tile.lo + rank * each) * p.rec, *b = p.B + (tile.matrix + tile.n0) * p.rec;
+            const uint32_t parts = base + L::kPartAt, own = base;      // the stages: idle once all has been multiplied
+            if (threadIdx.x == 0) mbar_arrive_expect_tx(bar(&ctrl->parts), static_cast<uint32_t>((split - 1) * mine * 512));
+            const int eb = BLOCK == 16 && n < cols ? mx_row_exp(b + n * static_cast<int64_t>(p.rec), exp_off) : 0;
+            int ea = BLOCK == 16 && lane < mine ? mx_row_exp(a + lane * static_cast<int64_t>(p.rec), exp_off) : 0;
+            bool ok = mbar_wait_bounded(bar(&ctrl->acc_full), done & 1);
+            ok = __all_sync(0xffffffffu, ok) && !aborted();
             tc_fence_after();
             if (ok) {
                 for (int c = 0; c < rows; c += 16) {
@@ -499,35 +520,68 @@ __global__ void __launch_bounds__(kNarrowThreads, 2) mx_narrow_kernel(const MxPr
                     tc_load16(tmem + (static_cast<uint32_t>(32 * warp) << 16) + c, v);
                     tc_load_wait(v);
 #pragma unroll
-                    for (int i = 0; i < 16; i++) part[(c + i) * 128 + 32 * warp + lane] = __uint_as_float(v[i]);
+                    for (int i = 0; i < 16; i++)
+                        asm volatile("st.shared.u32 [%0], %1;" ::"r"(own + ((c + i) * 128 + n) * 4), "r"(v[i]) : "memory");
                 }
+                fence_async_smem();
+            }
+            asm volatile("bar.sync 1, 128;" ::: "memory");
+            if (!pushed) cluster_wait();           // all CTAs have their barriers
+            if (ok && threadIdx.x < split && threadIdx.x != rank) {
+                const int to = threadIdx.x, n_to = min(each, rows - to * each), from = rank < to ? rank : rank - 1;
+                if (n_to > 0)
+                    cluster_push(cluster_at(parts + from * each * 512, to), own + to * each * 512, n_to * 512, cluster_at(bar(&ctrl->parts), to));
             }
             tc_fence_before();
-        }
-        cluster_barrier();
-        bool failed = false;
-        for (int q = 0; q < split; q++) failed = failed || cluster_load(smem_u32(&ctrl->abort), q) != 0;
-        if (threadIdx.x < 256 && !failed) {
-            for (int m = rank + split * (threadIdx.x >> 7); m < rows; m += 2 * split) {
-                const int ea = BLOCK == 16 ? mx_row_exp(a + m * static_cast<int64_t>(p.rec), exp_off) : 0;
-                uint32_t v[8];
-#pragma unroll
-                for (int q = 0; q < 8; q++) v[q] = q < split ? cluster_load(smem_u32(part + 128 * m + n), q) : 0;
-                float sum = __uint_as_float(v[0]);
-#pragma unroll
-                for (int q = 1; q < 8; q++) sum += __uint_as_float(v[q]);       // + 0 behind the last
-                if (n < cols) store_y(p, (tile.lo + m) * p.N + tile.n0 + n, BLOCK == 16 ? scaled(sum, ea + eb) : sum);
+            if (!more) asm volatile("bar.arrive 2, 160;" ::: "memory");        // tensor memory may go
+            if (ok && mine > 0) {
+                ok = mbar_wait_bounded(bar(&ctrl->parts), done & 1);
+                ok = __all_sync(0xffffffffu, ok);
             }
+            const float *mine_at = reinterpret_cast<const float *>(base_ptr) + rank * each * 128 + n;
+            const float *parts_at = reinterpret_cast<const float *>(base_ptr + L::kPartAt) + n;
+            for (int k = 0; ok && k < mine; k += 4) {          // four tokens at a time: their loads overlap
+                float sum[4] = {};
+                for (int q = 0; q < split; q++) {
+                    const float *src = q == rank ? mine_at + k * 128 : parts_at + ((q < rank ? q : q - 1) * each + k) * 128;
+#pragma unroll
+                    for (int i = 0; i < 4; i++) sum[i] += k + i < mine ? src[i * 128] : 0.0f;
+                }
+#pragma unroll
+                for (int i = 0; i < 4; i++) {
+                    const int e = BLOCK == 16 ? eb + __shfl_sync(0xffffffffu, ea, k + i) : 0;
+                    if (k + i < mine && n < cols) store_y(p, (tile.lo + rank * each + k + i) * p.N + tile.n0 + n, BLOCK == 16 ? scaled(sum[i], e) : sum[i]);
+                }
+            }
+            if (!ok && lane == 0) give_up();
+            done++;
+        } else if (!pushed) {
+            cluster_wait();
         }
-        fence_async_smem();       // the next tile's copies come after these reads
-        cluster_barrier();        // and nobody leaves while others read its memory
-        if (failed) break;
+        pushed = true;
+        if (!more) break;
+        fence_async_smem();       // the next tile's copies come after these reads, and its sums when all have read theirs
+        asm volatile("barrier.cluster.arrive;\n\tbarrier.cluster.wait;" ::: "memory");
     }
-    tc_fence_before();
-    __syncthreads();
-    if (warp == 9) {
-        tc_fence_after();
-        tc_free<false, L::kColumns>(tmem);
+    if (p.split > 1) {
+        if (!pushed) {            // no tile for this cluster
+            cluster_wait();
+            if (warp < 4) asm volatile("bar.arrive 2, 160;" ::: "memory");
+        }
+        cluster_arrive();         // nobody leaves while another CTA may push to it
+        if (warp == 13) {
+            asm volatile("bar.sync 2, 160;" ::: "memory");
+            tc_fence_after();
+            tc_free<false, L::kColumns>(tmem);
+        }
+        cluster_wait();
+    } else {
+        tc_fence_before();
+        __syncthreads();
+        if (warp == 13) {
+            tc_fence_after();
+            tc_free<false, L::kColumns>(tmem);
+        }
     }
 }
 
@@ -556,8 +610,51 @@ struct WideCtrl {
     int abort;
 };
 
+// `rows` rows of 128 bytes of Y from shared memory (16-byte piece q of row r at q ^ (r mod 8)) to rows of `cols` values that start
+// at `at` and are p.N values apart.
+__device__ __forceinline__ void store_turn(const MxProductParams &p, uint32_t turn, int rows, int64_t at, int cols) {
+    const int lane = threadIdx.x & 31;
+    if (p.y_maps) {               // rows of whole 16-byte pieces: eight lanes a row
+        const int esize = p.y_type == RAC_MX_FP32 ? 4 : 2, q = lane & 7;
+        uint8_t *const y = static_cast<uint8_t *>(p.Y) + at * esize + 16 * q;
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            const int r = 4 * i + (lane >> 3);
+            if (r < rows && q * 16 < cols * esize) *reinterpret_cast<uint4 *>(y + r * p.N * esize) = lds128(turn + r * 128 + (q ^ (r & 7)) * 16);
+        }
+    } else if (p.y_type == RAC_MX_FP32) {
+        float *const y = static_cast<float *>(p.Y) + at + lane;
+#pragma unroll 8
+        for (int r = 0; r < rows; r++)
+            if (lane < cols) y[r * p.N] = __uint_as_float(lds32(turn + r * 128 + ((lane >> 2) ^ (r & 7)) * 16 + (lane & 3) * 4));
+    } else {
+        // Two values a store wherever a row starts: a row at an odd place begins with the second half of a word.  Eight rows at a
+        // time, so that their loads, shuffles and stores overlap (one at a time: 42 us for 2051 x 2887 x 4096, 20 where N is 2888).
+        uint16_t *const y = static_cast<uint16_t *>(p.Y);
+        for (int r0 = 0; r0 < rows; r0 += 8) {
+            uint32_t w[8], before[8];                                                                // values 2 lane, 2 lane + 1
+#pragma unroll
+            for (int i = 0; i < 8; i++) w[i] = lds32(turn + (r0 + i) * 128 + ((lane >> 2) ^ i) * 16 + (lane & 3) * 4);
+#pragma unroll
+            for (int i = 0; i < 8; i++) before[i] = __shfl_up_sync(0xffffffffu, w[i], 1);
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                const int64_t to = at + (r0 + i) * p.N;
+                const int odd = static_cast<int>(to & 1), c = 2 * lane - odd;
+                const uint32_t two = odd ? __funnelshift_l(before[i], w[i], 16) : w[i];              // values c, c + 1
+                if (r0 + i < rows) {
+                    if (c >= 0 && c + 1 < cols) *reinterpret_cast<uint32_t *>(y + to + c) = two;
+                    else if (c >= 0 && c < cols) y[to + c] = static_cast<uint16_t>(two);
+                    else if (c < 0) y[to] = static_cast<uint16_t>(w[i]);
+                    if (odd && lane == 31 && cols == 64) y[to + 63] = static_cast<uint16_t>(w[i] >> 16);
+                }
+            }
+        }
+    }
+}
+
 template <int BLOCK, int QROWS>
-__global__ void __launch_bounds__(kWideThreads, 1) mx_wide_kernel(const MxProductParams p, const __grid_constant__ MxMaps maps) {
+__global__ void __launch_bounds__(kThreads, 1) mx_wide_kernel(const MxProductParams p, const __grid_constant__ MxMaps maps) {
     using L = WideLayout<BLOCK, QROWS>;
     constexpr int kWords = Scales<BLOCK>::kWords;
     extern __shared__ uint8_t raw[];
@@ -583,14 +680,15 @@ __global__ void __launch_bounds__(kWideThreads, 1) mx_wide_kernel(const MxProduc
         ctrl->abort = 0;
         mbar_init_fence();
     }
+    if (p.early) grid_launch_dependents();
     if (warp == 12 && lane < 4 + p.y_maps) tma_prefetch(&maps.a + lane);
     if (warp == 13) tc_alloc<true, L::kColumns>(smem_u32(&ctrl->tmem));
     tc_fence_before();
     __syncthreads();
-    cluster_barrier();                                   // the other CTA's barriers are there
+    cluster_arrive();                                    // this CTA's barriers are there, and the other's
+    cluster_wait();
     tc_fence_after();
     const uint32_t tmem = ctrl->tmem;
-    grid_dependency_wait();
 
     const int64_t first = blockIdx.x / 2, step = gridDim.x / 2;
     auto give_up = [&]() {
@@ -599,13 +697,17 @@ __global__ void __launch_bounds__(kWideThreads, 1) mx_wide_kernel(const MxProduc
     };
     auto aborted = [&]() { return *reinterpret_cast<volatile int *>(&ctrl->abort) != 0; };
     TileWalk<2 * kRows, QROWS> walk;
+    Tile head;                  // the first tile, worked out before the wait where it takes no memory to know it
+    if (!p.seg_off) head = walk.at(p, first);
+    grid_dependency_wait();
+    if (p.seg_off) head = walk.at(p, first);
     bool ok = true;
     int it = 0, done = 0, group = 0;       // stages, tiles and scale copies that this role has gone through
 
     if (warp == 12) {
         // ---- TMA
         for (int64_t t = first; ok; t += step) {
-            const Tile tile = walk.at(p, t);
+            const Tile tile = t == first ? head : walk.at(p, t);
             if (!tile.valid) break;
             if (lane == 0) {
                 const int row_a = static_cast<int>(min(tile.lo + rank * kRows, p.M)), row_b = static_cast<int>(tile.matrix + tile.n0);
@@ -641,7 +743,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) mx_wide_kernel(const MxProduc
     } else if (warp == 13) {
         // ---- matrix instructions, for both CTAs
         for (int64_t t = first; ok && rank == 0; t += step, done++) {
-            const Tile tile = walk.at(p, t);
+            const Tile tile = t == first ? head : walk.at(p, t);
             if (!tile.valid) break;
             if (lane == 0) {
                 const int ab = done % L::kAccs;
@@ -671,17 +773,22 @@ __global__ void __launch_bounds__(kWideThreads, 1) mx_wide_kernel(const MxProduc
         const int team = (warp - 4) >> 2;
         const int turn = lane >> 1 & 3;              // 64-byte swizzle: 16-byte piece c of row r lies at c ^ (r / 2 mod 4)
         for (int64_t t = first; ok; t += step) {
-            const Tile tile = walk.at(p, t);
+            const Tile tile = t == first ? head : walk.at(p, t);
             if (!tile.valid) break;
             for (int ks = 0; ks < p.k_stages; ks++, it++) {
                 const int st = it % L::kStages, sub = ks % L::kGroup, sb = group & 1;
                 const bool last = sub == L::kGroup - 1 || ks == p.k_stages - 1;
+                // both teams wait for every copy of scales: one that left a copy out could take its phase for the next but one
+                // (stages come in fours, so that each team sees every phase of its own)
+                if (sub == 0) ok = mbar_wait_bounded(bar(&ctrl->scale_full[sb]), group >> 1 & 1);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
                 group += last;
                 if ((it & 1) != team) {
                     if (last && lane == 0) mbar_arrive(bar(&ctrl->scale_empty[sb]));
                     continue;
                 }
-                ok = mbar_wait_bounded(bar(&ctrl->scale_full[sb]), (group - last) >> 1 & 1) && mbar_wait_bounded(bar(&ctrl->full[st]), it / L::kStages & 1);
+                ok = mbar_wait_bounded(bar(&ctrl->full[st]), it / L::kStages & 1);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 tc_fence_after();
@@ -724,7 +831,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) mx_wide_kernel(const MxProduc
         const int per = wide_y ? 32 : 64;          // values of a row of Y per turn
         int turns = 0;
         for (int64_t t = first; ok; t += step, done++) {
-            const Tile tile = walk.at(p, t);
+            const Tile tile = t == first ? head : walk.at(p, t);
             if (!tile.valid) break;
             const int64_t row0 = tile.lo + rank * kRows;
             const int rows = static_cast<int>(max(static_cast<int64_t>(0), min(tile.hi - row0, static_cast<int64_t>(kRows))));
@@ -813,22 +920,9 @@ __global__ void __launch_bounds__(kWideThreads, 1) mx_wide_kernel(const MxProduc
                         bulk_commit();
                     }
                 } else {
-                    // rows that are not all this segment's, or that start where TMA cannot: a row at a time
+                    // rows that are not all this segment's, or that start where TMA cannot
                     __syncwarp();
-                    for (int i = 0; i < mine; i++) {
-                        const int64_t at = (row0 + 32 * warp + i) * p.N + tile.n0 + c0;
-                        for (int c = lane; c < min(per, cols - c0); c += 32) {
-                            const int piece = c * (wide_y ? 4 : 2);
-                            const uint32_t src = turn + i * 128 + ((piece >> 4) ^ (i & 7)) * 16 + (piece & 15);
-                            if (wide_y) {
-                                static_cast<uint32_t *>(p.Y)[at + c] = lds32(src);
-                            } else {
-                                uint16_t v;
-                                asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(src));
-                                static_cast<uint16_t *>(p.Y)[at + c] = v;
-                            }
-                        }
-                    }
+                    store_turn(p, turn, mine, (row0 + 32 * warp) * p.N + tile.n0 + c0, min(per, cols - c0));
                     __syncwarp();
                 }
             }
@@ -841,7 +935,8 @@ __global__ void __launch_bounds__(kWideThreads, 1) mx_wide_kernel(const MxProduc
     }
     tc_fence_before();
     __syncthreads();
-    cluster_barrier();        // nobody leaves while the other's instructions read its memory or arrive at its barriers
+    cluster_arrive();
+    cluster_wait();           // nobody leaves while the other's instructions read its memory or arrive at its barriers
     if (warp == 13) {
         tc_fence_after();
         tc_free<true, L::kColumns>(tmem);
@@ -896,19 +991,26 @@ static int64_t weight_rows(const MxProductParams &p) { return p.seg_off ? p.n_se
 template <int BLOCK, int QROWS>
 static int launch_narrow(MxProductParams p, int sms, cudaStream_t s) {
     using L = NarrowLayout<QROWS>;
+    static_assert(L::part(2) <= L::kPart && L::part(3) <= L::kPart && L::part(4) <= L::kPart && L::part(5) <= L::kPart && L::part(6) <= L::kPart &&
+                  L::part(7) <= L::kPart && L::part(L::kMaxSplit) <= L::kPart && L::kPartAt >= QROWS * 512, "partial sums");
     MxMaps maps = {};
     if (!record_maps(&maps.a, &maps.a_scale, p.A, p.M, p, QROWS, 16, QROWS) ||
         !record_maps(&maps.b, &maps.b_scale, p.B, weight_rows(p), p, kRows, 16, kRows))
         return RAC_ECUDA;
     p.n_tiles = static_cast<int>((p.N + kRows - 1) / kRows);
-    const int64_t tiles = row_tiles(p, QROWS) * p.n_tiles, slots = 2 * sms;
+    const int64_t tiles = row_tiles(p, QROWS) * p.n_tiles;
+    // CTAs of clusters: one per SM where a tile is a few tokens (1 x 4096 x 4096: 128 CTAs 5.8 us, 256 6.1; 1 x 5120 x 5120: 120 CTAs
+    // 7.1, 240 7.4, 280, which do not all fit beside one another in clusters, 11.5), more where the tokens are work, too
+    // (64 x 5120 x 5120: 120 CTAs 12.2, 240 10.1).
+    const int64_t together = QROWS == 16 ? sms : sms * 5 / 3, slots = 2 * sms;
     p.split = 1;
-    while (p.split < 8 && tiles * p.split * 2 <= slots && p.split * 2 <= p.k_stages) p.split *= 2;
+    while (p.split < L::kMaxSplit && tiles * (p.split + 1) <= together && p.split < p.k_stages) p.split++;
     const int64_t ctas = p.split > 1 ? tiles * p.split : (tiles < slots ? tiles : slots);
+    p.early = p.split > 1;
     auto kernel = mx_narrow_kernel<BLOCK, QROWS>;
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kBytes) != cudaSuccess) return RAC_ECUDA;
-    if (p.split > 1) launch_cluster_after(kernel, static_cast<unsigned>(ctas), p.split, kNarrowThreads, L::kBytes, s, p, maps);
-    else launch_after(kernel, static_cast<unsigned>(ctas), kNarrowThreads, L::kBytes, s, p, maps);
+    if (p.split > 1) launch_cluster_after(kernel, static_cast<unsigned>(ctas), p.split, kThreads, L::kBytes, s, p, maps);
+    else launch_after(kernel, static_cast<unsigned>(ctas), kThreads, L::kBytes, s, p, maps);
     return cudaGetLastError() == cudaSuccess ? RAC_OK : RAC_ECUDA;
 }
 
@@ -926,9 +1028,10 @@ static int launch_wide(MxProductParams p, int sms, cudaStream_t s) {
         return RAC_ECUDA;
     p.n_tiles = static_cast<int>((p.N + QROWS - 1) / QROWS);
     const int64_t tiles = row_tiles(p, 2 * kRows) * p.n_tiles, pairs = sms / 2;
+    p.early = tiles <= pairs;
     auto kernel = mx_wide_kernel<BLOCK, QROWS>;
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kBytes) != cudaSuccess) return RAC_ECUDA;
-    launch_cluster_after(kernel, static_cast<unsigned>(2 * (tiles < pairs ? tiles : pairs)), 2, kWideThreads, L::kBytes, s, p, maps);
+    launch_cluster_after(kernel, static_cast<unsigned>(2 * (tiles < pairs ? tiles : pairs)), 2, kThreads, L::kBytes, s, p, maps);
     return cudaGetLastError() == cudaSuccess ? RAC_OK : RAC_ECUDA;
 }
 
@@ -936,12 +1039,17 @@ template <int BLOCK>
 static int dispatch_mx_product(const MxProductParams &p, cudaStream_t s) {
     const int sms = sm_count();
     if (sms <= 0) return RAC_ECUDA;
-    // rows per weight matrix, on average
-    const int64_t rows = (p.M + p.n_seg - 1) / p.n_seg;
-    if (rows > 128) return launch_wide<BLOCK, 256>(p, sms, s);
-    if (rows > 64) return launch_narrow<BLOCK, 128>(p, sms, s);
-    if (rows > 16) return launch_narrow<BLOCK, 64>(p, sms, s);
-    return launch_narrow<BLOCK, 16>(p, sms, s);
+    // By the rows that a weight matrix has, on average.  Few: their own width.  More: the narrow form where its tiles are few
+    // enough to be split among five CTAs or more (128 x 1024 x 4096: 8.0 us, wide 10.9), else tiles of 256 x 128 or 256 x 256,
+    // whichever takes less time in rounds of all pairs, a stage of the former taking 0.8 times as long as the latter's
+    // (256 x 5120 x 5120, one round of either: 12.9 and 14.8 us; 512 rows, two rounds and one: 20.5 and 15.0 us).
+    const int64_t rows = (p.M + p.n_seg - 1) / p.n_seg, pairs = sms / 2 > 0 ? sms / 2 : 1;
+    if (rows <= 16) return launch_narrow<BLOCK, 16>(p, sms, s);
+    if (rows <= 64 || row_tiles(p, 64) * ((p.N + kRows - 1) / kRows) <= sms / 3) return launch_narrow<BLOCK, 64>(p, sms, s);
+    const int64_t tall = row_tiles(p, 2 * kRows);
+    const int64_t rounds128 = (tall * ((p.N + 127) / 128) + pairs - 1) / pairs, rounds256 = (tall * ((p.N + 255) / 256) + pairs - 1) / pairs;
+    if (4 * rounds128 < 5 * rounds256) return launch_wide<BLOCK, 128>(p, sms, s);
+    return launch_wide<BLOCK, 256>(p, sms, s);
 }
 
 static int mx_product_impl(const rac_mx_cfg *cfg, const void *A, int64_t M, const int32_t *seg_off, int64_t n_seg, const void *B,

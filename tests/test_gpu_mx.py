@@ -442,3 +442,30 @@ def test_waits_that_cannot_complete_end_with_a_status(env, M, N, block):
     rac.rac_mx_product(cfg, A, M, B, N, Y, status)          # the device is as it was
     assert int(status) == 0
     check_product(Y, a, b, torch.bfloat16)
+
+
+@pytest.mark.parametrize("M,N,d,n", [(4000, 2048, 1280, 8), (2600, 700, 768, 40), (1500, 3000, 1280, 1), (3000, 5000, 256, 1), (60, 5000, 1792, 16),
+                                     (5000, 1000, 2304, 3)])
+@pytest.mark.parametrize("block", [16, 32])
+def test_calls_in_a_row_agree(env, M, N, d, n, block):
+    """Many tiles per CTA, odd and even numbers of stages, call after call: the same sums every time and no wait that runs out."""
+    rac, dev = env.rac, env.dev
+    A, a = operand(M, d, block, 3, dev)
+    B, b = operand(n * N, d, block, 4, dev)
+    cfg = rac.MxCfg(d, block)
+    off = [i * M // n for i in range(n + 1)]
+    seg_off = torch.tensor(off, dtype=torch.int32, device=dev)
+    status = torch.zeros(1, dtype=torch.int32, device=dev)
+    Ys = [torch.empty((M, N), dtype=torch.bfloat16, device=dev) for _ in range(2)]
+    for i in range(60):
+        Y = Ys[min(i, 1)]
+        if n == 1:
+            rac.rac_mx_product(cfg, A, M, B, N, Y, status)
+        else:
+            rac.rac_mx_product_segments(cfg, A, M, seg_off, n, B, N, Y, status)
+        if i == 0:
+            for s in range(n):
+                check_product(Y[off[s]:off[s + 1]], a[off[s]:off[s + 1]], b[s * N:(s + 1) * N], torch.bfloat16)
+        else:
+            assert torch.equal(Ys[0], Ys[1])
+    assert int(status) == 0
