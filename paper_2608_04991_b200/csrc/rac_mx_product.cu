@@ -628,8 +628,8 @@ __device__ __forceinline__ void store_turn(const MxProductParams &p, uint32_t tu
         for (int r = 0; r < rows; r++)
             if (lane < cols) y[r * p.N] = __uint_as_float(lds32(turn + r * 128 + ((lane >> 2) ^ (r & 7)) * 16 + (lane & 3) * 4));
     } else {
-        // Two values a store wherever a row starts: a row at an odd place begins with the second half of a word.  Eight rows at a
-        // time, so that their loads, shuffles and stores overlap (one at a time: 42 us for 2051 x 2887 x 4096, 20 where N is 2888).
+        // Two values a store wherever a row starts: the words between its first and last even places a row at a time, then what
+        // that leaves at either end, a lane for each row (ends within the rows' loop: 42 us for 2051 x 2887 x 4096).
         uint16_t *const y = static_cast<uint16_t *>(p.Y);
         for (int r0 = 0; r0 < rows; r0 += 8) {
             uint32_t w[8], before[8];                                                                // values 2 lane, 2 lane + 1
@@ -642,14 +642,18 @@ __device__ __forceinline__ void store_turn(const MxProductParams &p, uint32_t tu
                 const int64_t to = at + (r0 + i) * p.N;
                 const int odd = static_cast<int>(to & 1), c = 2 * lane - odd;
                 const uint32_t two = odd ? __funnelshift_l(before[i], w[i], 16) : w[i];              // values c, c + 1
-                if (r0 + i < rows) {
-                    if (c >= 0 && c + 1 < cols) *reinterpret_cast<uint32_t *>(y + to + c) = two;
-                    else if (c >= 0 && c < cols) y[to + c] = static_cast<uint16_t>(two);
-                    else if (c < 0) y[to] = static_cast<uint16_t>(w[i]);
-                    if (odd && lane == 31 && cols == 64) y[to + 63] = static_cast<uint16_t>(w[i] >> 16);
-                }
+                if (r0 + i < rows && c >= 0 && c + 1 < cols) *reinterpret_cast<uint32_t *>(y + to + c) = two;
             }
         }
+        auto value = [&](int c) {
+            uint16_t v;
+            asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(turn + lane * 128 + ((c >> 3) ^ (lane & 7)) * 16 + (c & 7) * 2));
+            return v;
+        };
+        const int64_t to = at + lane * p.N;
+        const int odd = static_cast<int>(to & 1);
+        if (lane < rows && odd) y[to] = value(0);
+        if (lane < rows && ((cols - odd) & 1)) y[to + cols - 1] = value(cols - 1);
     }
 }
 
