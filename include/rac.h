@@ -445,8 +445,9 @@ int rac_recon_error(const void *X, const void *X_hat, int64_t T, int32_t d, doub
  *     block 32   s = 2^k, k the smallest integer >= -127 with 6 * 2^k >= amax; byte = k + 127 (e8m0)
  *     block 16   r = the smallest integer >= -100 with 448 * 6 * 2^r >= amax of the row, 0 for a row of zeros;
  *                s = v * 2^r, v the smallest e4m3 number with 6 * v * 2^r >= amax; byte = v as e4m3 (bit 7 is zero)
- *     code       x / s rounded to the nearest e2m1 magnitude, to the even code of two that are equally near; the sign of x
- * A block of zeros has scale byte 0 and codes of magnitude 0.  A block that holds a NaN or an infinity has the scale byte
+ *     code       x / s rounded to the nearest e2m1 magnitude, to the even code of two that are equally near; the sign of x, none
+ *                where the magnitude is 0
+ * A block of zeros has scale byte 0 and codes 0.  A block that holds a NaN or an infinity has the scale byte
  * of NaN (127 with block 16, 255 with block 32) and codes 0, and does not count towards r: it decodes to NaN, makes the
  * row of a product NaN, and leaves every other block alone.  A row depends on nothing but itself: any range of rows is a contiguous byte
  * range, and rows may be coded in any split into calls.

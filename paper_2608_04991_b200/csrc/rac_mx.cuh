@@ -35,6 +35,12 @@ inline bool mx_overlap(const void *a, size_t na, const void *b, size_t nb) {
     return na > 0 && nb > 0 && a0 < b0 + nb && b0 < a0 + na;
 }
 
+inline int mx_sm_count() {
+    int dev = 0, n = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
+    return n;
+}
+
 // 2^e for e in -126..127
 __device__ __forceinline__ float mx_pow2(int e) { return __uint_as_float(static_cast<uint32_t>(e + 127) << 23); }
 // an e8m0 byte below 255

@@ -980,11 +980,6 @@ static bool record_maps(CUtensorMap *codes, CUtensorMap *scales, const uint8_t *
                       scale_width == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_NONE);
 }
 
-static int sm_count() {
-    int dev = 0, n = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
-    return n;
-}
 // Tiles of `rows` rows of A, at most: with segments the lengths are on the device, and each may end in a tile that is not full.
 static int64_t row_tiles(const MxProductParams &p, int rows) {
     if (!p.seg_off) return (p.M + rows - 1) / rows;
@@ -1041,7 +1036,7 @@ static int launch_wide(MxProductParams p, int sms, cudaStream_t s) {
 
 template <int BLOCK>
 static int dispatch_mx_product(const MxProductParams &p, cudaStream_t s) {
-    const int sms = sm_count();
+    const int sms = mx_sm_count();
     if (sms <= 0) return RAC_ECUDA;
     // By the rows that a weight matrix has, on average.  Few: their own width.  More: the narrow form where its tiles are few
     // enough to be split among five CTAs or more (128 x 1024 x 4096: 8.0 us, wide 10.9), else tiles of 256 x 128 or 256 x 256,

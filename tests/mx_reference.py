@@ -40,7 +40,7 @@ def encode(x, block):
     for i in range(1, 8):
         middle = (MAGNITUDE[i - 1] + MAGNITUDE[i]) / 2
         code += (y >= middle) if i % 2 == 0 else (y > middle)
-    code += 8 * np.signbit(b)
+    code += 8 * (np.signbit(b) & (code > 0))          # a magnitude of 0 has no sign
     code = np.where(fine[..., None], code, 0).reshape(T, d)
     out = np.zeros((T, record_bytes(d, block)), dtype=np.uint8)
     out[:, : d // 2] = code[:, 0::2] | code[:, 1::2] << 4

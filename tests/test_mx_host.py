@@ -115,4 +115,4 @@ def test_reference_rounds_to_the_nearest_code_and_clips_nothing(block):
     best = np.abs(all_codes * s[..., None] - x[..., None]).min(-1)
     assert np.array_equal(np.abs(v - x), best)
     assert (np.abs(x) <= 6 * s).all()
-    assert np.array_equal(np.signbit(v), np.signbit(x)) or (v[np.signbit(v) != np.signbit(x)] == 0).all()
+    assert np.array_equal(np.signbit(v), np.signbit(x) & (v != 0))
