@@ -17,6 +17,7 @@ struct MxParams {
     int tpr;                 // threads per row: d/16
     int wide;                // X and X_hat start at multiples of 32 bytes: a thread's values in one access
     int rows;                // rows per CTA and round
+    int each;                // rounds of a CTA (encode)
     int early;               // the next kernel on the stream may be set up from the start
 };
 
@@ -119,22 +120,23 @@ __global__ void __launch_bounds__(512, CHUNKS > 1 ? 1 : STAY ? 3 : 4) mx_encode_
     grid_dependency_wait();
     if (BLOCK == 16) __syncthreads();
 
-    const int64_t step = static_cast<int64_t>(gridDim.x) * p.rows;
-    int64_t row = static_cast<int64_t>(blockIdx.x) * p.rows + r;
+    // a CTA's rows lie behind one another
+    const int64_t step = p.rows, begin = static_cast<int64_t>(blockIdx.x) * p.each * p.rows, end = min(p.T, begin + static_cast<int64_t>(p.each) * p.rows);
+    int64_t row = begin + r;
     Piece next[CHUNKS];
     auto fetch = [&](int64_t at) {
 #pragma unroll
         for (int k = 0; k < CHUNKS; k++) {
             const int c = c0 + k * blockDim.x;
-            if (r < p.rows && at < p.T && (CHUNKS == 1 || c < p.tpr)) next[k] = load_piece(p.X + (at * p.d + 16 * static_cast<int64_t>(c)) * 2, wide);
+            if (r < p.rows && at < end && (CHUNKS == 1 || c < p.tpr)) next[k] = load_piece(p.X + (at * p.d + 16 * static_cast<int64_t>(c)) * 2, wide);
             else next[k] = Piece{};
         }
     };
     fetch(row);
     int slot = 0;
     uint32_t any_bad = 0;
-    for (int64_t row0 = static_cast<int64_t>(blockIdx.x) * p.rows; row0 < p.T; row0 = STAY ? row0 + step : p.T, row += step) {
-        const bool live = r < p.rows && row < p.T;
+    for (int64_t row0 = begin; row0 < end; row0 = STAY ? row0 + step : end, row += step) {
+        const bool live = r < p.rows && row < end;
         Piece x[CHUNKS];
         uint32_t amax[CHUNKS];
         uint32_t bad = 0, most = 0;
@@ -288,6 +290,7 @@ static int mx_shape(const MxGeometry &g, int64_t T, const void *X, const void *X
     const int64_t groups = (T + p->rows - 1) / p->rows;
     int64_t each = groups * *threads / (static_cast<int64_t>(sms) * 2048 * 2);       // two full rounds of the SMs at least
     each = each < 3 ? 1 : each > rounds ? rounds : each;
+    p->each = static_cast<int>(each);
     *grid = static_cast<unsigned>((groups + each - 1) / each);
     p->early = groups * *threads <= static_cast<int64_t>(sms) * 1024;
     return RAC_OK;
@@ -296,7 +299,7 @@ static int mx_shape(const MxGeometry &g, int64_t T, const void *X, const void *X
 template <bool HALF, int BLOCK, bool XHAT>
 static void launch_mx_encode(const MxParams &p, unsigned grid, unsigned threads, cudaStream_t s) {
     const size_t smem = BLOCK == 16 ? 3 * sizeof(uint32_t) * p.rows : 0;
-    const bool stay = static_cast<int64_t>(grid) * p.rows < p.T;
+    const bool stay = p.each > 1;
     if (p.tpr > 1024) stay ? launch_after(mx_encode_kernel<HALF, BLOCK, XHAT, 4, true>, grid, threads, smem, s, p)
                            : launch_after(mx_encode_kernel<HALF, BLOCK, XHAT, 4, false>, grid, threads, smem, s, p);
     else if (p.tpr > 512) stay ? launch_after(mx_encode_kernel<HALF, BLOCK, XHAT, 2, true>, grid, threads, smem, s, p)
