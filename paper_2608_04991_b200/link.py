@@ -160,6 +160,37 @@ class DeviceCodec:
             raise RuntimeError(f"device status {s:#x}")
 
 
+class EntryProduct:
+    """The first projection behind the boundary: what an end reconstructed, as microscaled 4-bit records, times a weight
+    matrix [N, d] (bf16 on the device) whose records are laid out once."""
+
+    def __init__(self, W: torch.Tensor, block: int = 16):
+        from . import binding as rac
+        self.rac = rac
+        self.N, d = W.shape
+        self.cfg = rac.MxCfg(d, block)
+        self.rec = rac.rac_mx_record_bytes(self.cfg)
+        self.status = torch.zeros(1, dtype=torch.int32, device=W.device)
+        self.records = self._encode(W)
+        self.check()
+
+    def _encode(self, X: torch.Tensor) -> torch.Tensor:
+        records = torch.empty((X.shape[0], self.rec), dtype=torch.uint8, device=X.device)
+        self.rac.rac_mx_encode(self.cfg, X, X.shape[0], records, records.numel(), None, self.status)
+        return records
+
+    def __call__(self, x_hat: torch.Tensor) -> torch.Tensor:
+        T = x_hat.shape[0]
+        Y = torch.empty((T, self.N), dtype=torch.bfloat16, device=x_hat.device)
+        self.rac.rac_mx_product(self.cfg, self._encode(x_hat), T, self.records, self.N, Y, self.status)
+        return Y
+
+    def check(self) -> None:
+        s = int(self.status.item())
+        if s:
+            raise RuntimeError(f"device status {s:#x}")
+
+
 # ------------------------------------------------------------------------------------------------ endpoints
 @dataclass
 class LinkStats:
@@ -256,6 +287,12 @@ class Receiver(_End):
         self.x_hat = self.codec.decode_reconstruct(payload, T, self.states, self.n_hist, ref_row)
         return self.x_hat
 
+    def enter(self, entry: EntryProduct) -> torch.Tensor:
+        """The receiving partition's first projection of the request in flight."""
+        if self.x_hat is None:
+            raise RuntimeError("no request in flight")
+        return entry(self.x_hat)
+
     def downlink(self, Y: torch.Tensor) -> torch.Tensor:
         """Codes Y against the uplink reconstruction (identity rows); returns what the sender will reconstruct."""
         T = Y.shape[0]
@@ -298,6 +335,8 @@ def _demo(argv=None) -> None:
     ap.add_argument("--bits", type=int, default=4)
     ap.add_argument("--group", type=int, default=128)
     ap.add_argument("--topk-group", type=int, default=1)
+    ap.add_argument("--entry", type=int, default=0, metavar="N",
+                    help="the receiver also takes its first projection, to N features, of every request")
     ap.add_argument("--check", action="store_true",
                     help="fail (exit status 1) unless both ends hold the same reconstructed history at the end: their "
                          "digests travel over the process group and are compared on both ranks")
@@ -316,6 +355,10 @@ def _demo(argv=None) -> None:
     wl = synth.request_stream(a.requests, a.tokens, seed=77)
     scale = synth.channel_scale(a.d, 77, dev)
     end = Sender(codec, link) if rank == 0 else Receiver(codec, link)
+    entry = None
+    if a.entry and rank == 1:
+        gen = synth.generator(78, dev)
+        entry = EntryProduct((torch.randn((a.entry, a.d), generator=gen, device=dev) * a.d ** -0.5).to(torch.bfloat16))
     t0, t1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
     t0.record()
     for r in range(a.requests):
@@ -328,9 +371,13 @@ def _demo(argv=None) -> None:
             end.downlink()
         else:
             x_hat = end.uplink()
+            if entry is not None:
+                end.enter(entry)
             end.downlink(synth.drifted_state(x_hat, gen))
     t1.record()
     torch.cuda.synchronize()
+    if entry is not None:
+        entry.check()
     digest = torch.tensor([states_digest(end.states, end.n_hist)], dtype=torch.int64, device=dev)
     both = [torch.zeros_like(digest) for _ in range(2)]
     dist.all_gather(both, digest)

@@ -3,7 +3,8 @@
 For every candidate configuration the sender path is run on the given activations (step tables from
 ``rac_calibrate_steps`` where the configuration needs them, then ``rac_encode_reconstruct``) and the packed bytes per
 token are reported beside the reconstruction error (``rac_recon_error``).  Members with shared coefficient pairs
-(``coef_fmt = 1``) run ``rac_fit_segments`` first and count their shared words towards the bytes.  Picking a
+(``coef_fmt = 1``) run ``rac_fit_segments`` first and count their shared words towards the bytes.  The microscaled 4-bit
+records, which code a state without any reference, stand beside them.  Picking a
 configuration against a model-quality target needs the model and its evaluation suites and is not done here.
 
 Every step runs in the CUDA kernels of the C-ABI library; this module only loops over configurations.
@@ -102,6 +103,42 @@ def sweep(X: torch.Tensor, ref_base: Optional[torch.Tensor], ref_row: Optional[t
     return out
 
 
+def sweep_direct(X: torch.Tensor, blocks: Iterable[int] = (16, 32), reps: int = 3) -> List[dict]:
+    """The microscaled 4-bit records (``rac_mx_encode``: no reference, one scale per block) on the same scale as ``sweep``."""
+    dev = X.device
+    T, d = X.shape
+    x_hat = torch.empty_like(X)
+    status = torch.zeros(1, dtype=torch.int32, device=dev)
+    err = torch.zeros(3, dtype=torch.float64, device=dev)
+    ews_n = rac.rac_recon_error_workspace_bytes()
+    ews = torch.empty(ews_n, dtype=torch.uint8, device=dev)
+    out = []
+    for block in blocks:
+        cfg = rac.MxCfg(d, block, x_type=X.dtype)
+        rec = rac.rac_mx_record_bytes(cfg)
+        if rec == 0:
+            raise ValueError(f"unsupported configuration {cfg!r}")
+        pay = torch.empty(T * rec, dtype=torch.uint8, device=dev)
+        run = lambda: rac.rac_mx_encode(cfg, X, T, pay, pay.numel(), x_hat, status)
+        run()
+        e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        torch.cuda.synchronize()
+        e0.record()
+        for _ in range(reps):
+            run()
+        e1.record()
+        rac.rac_recon_error(X, x_hat, T, d, err, ews, ews_n)
+        torch.cuda.synchronize()
+        se, sx, mx = err.tolist()
+        out.append({
+            "direct": True, "group": 0, "bits": 4, "topk": 0, "scale_mode": -1, "qgroup": block, "topk_group": 0, "coef_fmt": 0,
+            "record_bytes": rec, "shared_bytes_per_token": 0.0, "payload_over_raw": rec / (2.0 * d),
+            "rel_rms_error": (se / sx) ** 0.5 if sx > 0 else 0.0, "max_abs_error": mx,
+            "encode_reconstruct_ms": e0.elapsed_time(e1) / reps, "status": int(status.item()),
+        })
+    return out
+
+
 def default_grid(d: int) -> List[rac.CodecCfg]:
     """Static-table members (per-token outliers) and Eq. 8 members (per-group outliers, 8-bit, one scale per token)."""
     cfgs = []
@@ -138,7 +175,7 @@ def main() -> int:
     gen = synth.generator(args.seed, dev)
     X = synth.activations(args.tokens, args.d, synth.channel_scale(args.d, args.seed, dev), gen)
     R = synth.affine_noisy_reference(X, 128, gen)
-    rows = sweep(X, R, None, default_grid(args.d))
+    rows = sweep(X, R, None, default_grid(args.d)) + sweep_direct(X)
     if args.segment > 0:
         # the reference of these members carries ONE affine map per (segment, group): what a shared pair can undo
         bounds = list(range(0, args.tokens, args.segment)) + [args.tokens]
@@ -165,8 +202,8 @@ def main() -> int:
               "coefficient pair per segment and group, outside the records")
     print(f"{'mode':>7} {'coef':>7} {'g_a':>4} {'g_q':>5} {'b':>2} {'k':>3} {'k_g':>3} {'bytes':>8} {'/raw':>6} {'rel rms':>9} {'max abs':>8} {'ms':>7}")
     for r in rows:
-        mode = "static" if r["scale_mode"] == 0 else "Eq.8"
-        coef = "shared" if r["coef_fmt"] == 1 else ("seg" if r.get("segmented") else "token")
+        mode = "e2m1" if r.get("direct") else "static" if r["scale_mode"] == 0 else "Eq.8"
+        coef = "none" if r.get("direct") else "shared" if r["coef_fmt"] == 1 else ("seg" if r.get("segmented") else "token")
         print(f"{mode:>7} {coef:>7} {r['group']:>4} {r['qgroup']:>5} {r['bits']:>2} {r['topk']:>3} {r['topk_group']:>3} "
               f"{r['record_bytes'] + r['shared_bytes_per_token']:>8.1f} {r['payload_over_raw']:>6.3f} {r['rel_rms_error']:>9.5f} "
               f"{r['max_abs_error']:>8.3f} {r['encode_reconstruct_ms']:>7.3f}")

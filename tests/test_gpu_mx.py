@@ -469,3 +469,43 @@ def test_calls_in_a_row_agree(env, M, N, d, n, block):
         else:
             assert torch.equal(Ys[0], Ys[1])
     assert int(status) == 0
+
+
+def test_receiver_enters_the_next_partition(env):
+    """The link's path: reconstruct what crossed, code it, first projection behind the boundary."""
+    from paper_2608_04991_b200 import link, synth
+    rac, dev = env.rac, env.dev
+    d, T, N = 1024, 200, 300
+    cfg = rac.CodecCfg(d, 128, 4, 0, scale_mode=1, topk_group=1)
+    a, b = link.Loopback.pair()
+    sender, receiver = link.Sender(link.DeviceCodec(cfg, dev, 2 * T), a), link.Receiver(link.DeviceCodec(cfg, dev, 2 * T, with_index=False), b)
+    gen = synth.generator(5, dev)
+    W = (torch.randn((N, d), generator=gen, device=dev) / 32).to(torch.bfloat16)
+    for block in (16, 32):
+        entry = link.EntryProduct(W, block)
+        with pytest.raises(RuntimeError, match="no request in flight"):
+            receiver.enter(entry)
+        X = synth.activations(T, d, synth.channel_scale(d, 5, dev), gen)
+        sender.uplink(torch.arange(T, dtype=torch.int32, device=dev), X)
+        x_hat = receiver.uplink()
+        Y = receiver.enter(entry)
+        entry.check()
+        values = [torch.from_numpy(ref.decode(ref.encode(v.double().cpu().numpy(), block)[0], d, block)).to(dev) for v in (x_hat, W)]
+        check_product(Y, values[0], values[1], torch.bfloat16)
+        sender.finish_without_downlink()
+        receiver.finish_without_downlink()
+
+
+@pytest.mark.parametrize("x", ["bf16"])
+def test_sweep_reports_the_direct_records(env, x):
+    from paper_2608_04991_b200 import sweep, synth
+    dev = env.dev
+    T, d = 300, 1024
+    X = synth.activations(T, d, synth.channel_scale(d, 6, dev), synth.generator(6, dev))
+    rows = sweep.sweep_direct(X)
+    v = X.double().cpu().numpy()
+    for block, r in zip((16, 32), rows):
+        e = typed(ref.decode(ref.encode(v, block)[0], d, block), x).double().numpy() - v
+        assert r["status"] == 0 and r["record_bytes"] == ref.record_bytes(d, block) and r["qgroup"] == block
+        assert abs(r["rel_rms_error"] - np.sqrt((e ** 2).sum() / (v ** 2).sum())) < 1e-9 and r["max_abs_error"] == np.abs(e).max()
+    assert rows[0]["rel_rms_error"] < rows[1]["rel_rms_error"]          # smaller blocks, finer scales
