@@ -493,8 +493,8 @@ int rac_mx_product(const rac_mx_cfg *cfg, const void *A, int64_t M, const void *
  *   seg_off  device int32[n_seg+1], ascending; equal neighbours = an empty segment.  The lengths stay on the device.
  *   B        records of n_seg*N rows: matrix s is the rows s*N .. s*N+N
  * Rows of Y that no segment holds (before seg_off[0], from seg_off[n_seg] on) are left as they are.  Offsets outside
- * [0, M] are clipped into it and a segment whose end lies before its start is empty; where segments overlap, the
- * overlapping rows hold the product of one of them.  n_seg at most 65535, n_seg*N below 2^31. */
+ * [0, M] are clipped into it and a segment whose end lies before its start is empty; where segments overlap, the values
+ * of the overlapping rows come from one or the other of them.  n_seg at most 65535, n_seg*N below 2^31. */
 int rac_mx_product_segments(const rac_mx_cfg *cfg, const void *A, int64_t M, const int32_t *seg_off, int64_t n_seg,
                             const void *B, int64_t N, void *Y, uint32_t *dev_status, void *stream);
 

@@ -509,3 +509,89 @@ def test_sweep_reports_the_direct_records(env, x):
         assert r["status"] == 0 and r["record_bytes"] == ref.record_bytes(d, block) and r["qgroup"] == block
         assert abs(r["rel_rms_error"] - np.sqrt((e ** 2).sum() / (v ** 2).sum())) < 1e-9 and r["max_abs_error"] == np.abs(e).max()
     assert rows[0]["rel_rms_error"] < rows[1]["rel_rms_error"]          # smaller blocks, finer scales
+
+
+@pytest.mark.parametrize("M,N,d", [(300, 300, 160), (2000, 131, 992)])
+def test_row_exponents_at_their_ends_in_large_products(env, M, N, d):
+    """The large tiles apply the exponents apart from one another where a single factor would not hold them."""
+    rac, dev = env.rac, env.dev
+    A, _ = operand(M, d, 16, 1, dev)
+    B, _ = operand(N, d, 16, 2, dev)
+    A[:, d // 2 + d // 16] = 110
+    B[:, d // 2 + d // 16] = 256 - 100
+    A[5:9, d // 2 + d // 16] = 256 - 20
+    a, b = (torch.from_numpy(ref.decode(R.cpu().numpy(), d, 16)).to(dev) for R in (A, B))
+    for p, q, u, v, m, n in ((A, B, a, b, M, N), (B, A, b, a, N, M)):
+        Y = torch.empty((m, n), dtype=torch.float32, device=dev)
+        rac.rac_mx_product(rac.MxCfg(d, 16, y_type=torch.float32), p, m, q, n, Y, None)
+        check_product(Y, u, v, torch.float32)
+
+
+@pytest.mark.parametrize("block", [16, 32])
+@pytest.mark.parametrize("M,N,d,off", [(40, 100, 1024, [0, 40, 0, 40, 0, 40]), (200, 100, 1536, [0, 200, 0, 200, 0, 200, 0, 200]),
+                                       (900, 300, 512, [0, 900, 0, 900])])
+def test_segments_that_overlap_and_share_a_matrix(env, M, N, d, off, block):
+    """More tiles than the sizes promise, in the form that splits the channels over clusters too."""
+    rac, dev = env.rac, env.dev
+    n = len(off) - 1
+    A, a = operand(M, d, block, 1, dev)
+    B, b = operand(N, d, block, 2, dev)
+    Y = torch.full((M, N), 77.0, dtype=torch.bfloat16, device=dev)
+    status = torch.zeros(1, dtype=torch.int32, device=dev)
+    for _ in range(5):
+        rac.rac_mx_product_segments(rac.MxCfg(d, block), A, M, torch.tensor(off, dtype=torch.int32, device=dev), n, B.repeat(n, 1), N, Y, status)
+        check_product(Y, a, b, torch.bfloat16)
+        Y.fill_(77)
+    assert int(status) == 0
+
+
+@pytest.mark.parametrize("block", [16, 32])
+@pytest.mark.parametrize("T,d", [(5, 96), (70, 2880), (400, 544)])
+def test_buffers_that_start_at_16_bytes_only(env, T, d, block):
+    """Every pointer a multiple of 16 bytes and of no more."""
+    rac, dev = env.rac, env.dev
+    cfg = rac.MxCfg(d, block)
+    rec = rac.rac_mx_record_bytes(cfg)
+
+    def at16(shape, dtype):
+        n = int(np.prod(shape)) * torch.empty((), dtype=dtype).element_size()
+        raw = torch.zeros(n + 64, dtype=torch.uint8, device=dev)
+        skip = (16 - raw.data_ptr()) % 32
+        v = raw[skip: skip + n].view(dtype).view(shape)
+        assert v.data_ptr() % 32 == 16
+        return v
+    X, xh, out, pay = at16((T, d), torch.bfloat16), at16((T, d), torch.bfloat16), at16((T, d), torch.bfloat16), at16((T, rec), torch.uint8)
+    X.copy_(states(T, d, "bf16", 1, dev).clamp(-1e4, 1e4))
+    rac.rac_mx_encode(cfg, X, T, pay, pay.numel(), xh, None)
+    want, _ = ref.encode(X.double().cpu().numpy(), block)
+    values = ref.decode(want, d, block)
+    assert np.array_equal(pay.cpu().numpy(), want) and same_bits(xh, typed(values, "bf16"))
+    rac.rac_mx_decode(cfg, pay, T, out, None)
+    assert same_bits(out, xh)
+    a = torch.from_numpy(values).to(dev)
+    for N in (T, T // 2):
+        Y = at16((T, N), torch.bfloat16)
+        rac.rac_mx_product(cfg, pay, T, pay, N, Y, None)
+        check_product(Y, a, a[:N], torch.bfloat16)
+
+
+def test_a_long_encode_in_place_and_odd_counts(env):
+    """CTAs that go through several rows: the last ones of a count that no split divides, in place."""
+    rac, dev = env.rac, env.dev
+    for T, d, block in ((20011, 1056, 16), (20011, 1056, 32), (9001, 4128, 16), (4999, 16416, 16), (200003, 96, 16)):
+        X = torch.randn((T, d), generator=torch.Generator(device=dev).manual_seed(T), device=dev).to(torch.bfloat16)
+        cfg = rac.MxCfg(d, block)
+        pay = torch.empty((T, rac.rac_mx_record_bytes(cfg)), dtype=torch.uint8, device=dev)
+        Y = X.clone()
+        rac.rac_mx_encode(cfg, Y, T, pay, pay.numel(), Y, None)
+        pick = torch.cat((torch.arange(0, 40), torch.arange(T // 2, T // 2 + 40), torch.arange(T - 80, T))).to(dev)
+        want, _ = ref.encode(X[pick].double().cpu().numpy(), block)
+        assert np.array_equal(pay[pick].cpu().numpy(), want)
+        out = torch.empty_like(X)
+        rac.rac_mx_decode(cfg, pay, T, out, None)
+        assert same_bits(out, Y)
+        few = torch.empty_like(pay)                     # the same records from calls of other sizes
+        for t in range(0, T, 4096):
+            n = min(4096, T - t)
+            rac.rac_mx_encode(cfg, X[t:t + n], n, few[t:t + n], n * few.shape[1], None, None)
+        assert torch.equal(few, pay)
