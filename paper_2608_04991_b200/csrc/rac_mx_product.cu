@@ -2,21 +2,22 @@
 //
 // The tensor cores take the records' codes and block scales as they stand (tcgen05.mma with block scaling, 64 channels an
 // instruction): codes travel by TMA from the records to shared memory in 128-byte swizzled tiles, 256 channels of a row at a
-// time, scale bytes by TMA too; four warps, one for each quarter of tensor memory's lanes, carry the scales from shared to
+// time, scale bytes by TMA too; eight warps, two for each quarter of tensor memory's lanes, carry the scales from shared to
 // tensor memory (tcgen05.st), where lane i holds beside one another the scales of rows i, i+32, i+64 and i+96.  The
 // copy instruction made for this (tcgen05.cp) takes its turn between the matrix instructions and held them up: 384 us
-// against 220 us without any scales for 16384 x 5120 x 5120.  Sums stay in tensor memory in binary32.  The row exponents of
-// block 16 are powers of two and commute with the sum: the epilogue applies them.
+// against 220 us without any scales for 16384 x 5120 x 5120 (tiles of single CTAs, no epilogue).  Sums stay in tensor memory
+// in binary32.  The row exponents of block 16 are powers of two and commute with the sum: the epilogue applies them.
 //
 // Two shapes of work.
 //   wide    many rows: a pair of CTAs makes a tile of 256 rows of A by 256 (128) of B with cta_group::2, so that each CTA loads
-//           half of either operand.  Rows of A are the lanes of the accumulator: a thread holds consecutive values of a row
-//           of Y.  Persistent pairs.  What bounds it is the way from L2 to shared memory: 128 x 256 tiles of single CTAs
-//           (54 KB for what is 38 KB per CTA here) took 214 us with all but one of every four matrix instructions left out.
-//   narrow  few rows (a decode step, a segment of a few tokens): a tile is 128 rows of B by up to 128 of A, so the weights
-//           fill the 128 lanes and a handful of tokens costs a handful of columns.  What bounds it is reading the weights;
+//           half of either operand (38 KB a stage, 54 KB for a tile of 128 x 256 by one CTA, whose loads alone took 214 us of the
+//           size above).  Rows of A are the lanes of the accumulator: a thread holds consecutive values of a row of Y.
+//           Persistent pairs.  210 us (4.1 PFLOP/s) in short bursts; in a sustained run the power limit holds it at 256 us.
+//   narrow  few rows (a decode step, a segment of a few tokens): a tile is 128 rows of B by up to 64 of A, so the weights
+//           fill the 128 lanes and a handful of tokens costs a handful of columns.  What bounds it is the weights' way in, a
+//           ring of copies whose round trips are 1.5 to 2.5 us, and for a single token the set-up and the sums' exchange;
 //           where the tiles alone do not fill the SMs, clusters split the channels and add their partial sums through
-//           distributed shared memory in a fixed order.
+//           distributed shared memory in a fixed order.  1 x 4096 x 4096: 6.6 us; 64 x 5120 x 5120: 10.6 us.
 // Warps 0-3 of a CTA are the epilogue, 4-11 carry scales, the next issues TMA loads and the last the matrix
 // instructions.  Every wait on an mbarrier is bounded: a copy that never lands ends the kernel with RAC_STATUS_TIMEOUT.
 #include <cuda.h>
@@ -194,8 +195,24 @@ struct Tile {
 };
 template <int MROWS, int NROWS>
 struct TileWalk {
-    int64_t before = 0;   // tiles along M of the segments before `s`
-    int s = 0;
+    // 32 segments at a time, one a lane: its rows and the tiles along M up to its end
+    int s = -32, lo = 0, hi = 0;
+    int64_t sum = 0;
+    __device__ __forceinline__ void load(const MxProductParams &p, int64_t before) {
+        const int at = s + (threadIdx.x & 31);
+        lo = hi = 0;
+        if (at < p.n_seg) {
+            lo = max(p.seg_off[at], 0);
+            hi = static_cast<int>(min(static_cast<int64_t>(p.seg_off[at + 1]), p.M));
+        }
+        sum = hi > lo ? (static_cast<int64_t>(hi) - lo + MROWS - 1) / MROWS : 0;
+#pragma unroll
+        for (int o = 1; o < 32; o *= 2) {
+            const int64_t v = __shfl_up_sync(0xffffffffu, sum, o);
+            if ((threadIdx.x & 31) >= o) sum += v;
+        }
+        sum += before;
+    }
     __device__ __forceinline__ Tile at(const MxProductParams &p, int64_t t) {
         Tile r;
         const int64_t mt = t <= INT32_MAX ? static_cast<int32_t>(t) / p.n_tiles : t / p.n_tiles;
@@ -207,37 +224,30 @@ struct TileWalk {
             r.valid = r.lo < p.M;
             return r;
         }
-        const int lane = threadIdx.x & 31;
         r.valid = false;
         r.lo = r.hi = r.matrix = 0;
-        while (s < p.n_seg) {
-            int64_t lo = 0, hi = 0;
-            if (s + lane < p.n_seg) {
-                lo = max(p.seg_off[s + lane], 0);
-                hi = min(static_cast<int64_t>(p.seg_off[s + lane + 1]), p.M);
-            }
-            const int64_t n = hi > lo ? (hi - lo + MROWS - 1) / MROWS : 0;
-            int64_t sum = n;
-#pragma unroll
-            for (int o = 1; o < 32; o *= 2) {
-                const int64_t v = __shfl_up_sync(0xffffffffu, sum, o);
-                if (lane >= o) sum += v;
-            }
-            const uint32_t behind = __ballot_sync(0xffffffffu, before + sum > mt);
+        if (s < 0) {
+            s = 0;
+            load(p, 0);
+        }
+        for (;;) {
+            const uint32_t behind = __ballot_sync(0xffffffffu, sum > mt);
             if (behind) {
                 const int l = __ffs(behind) - 1;
-                before += __shfl_sync(0xffffffffu, sum - n, l);
-                s += l;
-                r.lo = __shfl_sync(0xffffffffu, lo, l) + (mt - before) * MROWS;
                 r.hi = __shfl_sync(0xffffffffu, hi, l);
-                r.matrix = static_cast<int64_t>(s) * p.N;
+                // tiles are counted from the segment's end: the last one is the one that may not be full
+                const int first = __shfl_sync(0xffffffffu, lo, l);
+                const int64_t tiles = (r.hi - first + MROWS - 1) / MROWS;
+                r.lo = first + (tiles - (__shfl_sync(0xffffffffu, sum, l) - mt)) * MROWS;
+                r.matrix = static_cast<int64_t>(s + l) * p.N;
                 r.valid = true;
                 return r;
             }
-            before += __shfl_sync(0xffffffffu, sum, 31);
+            if (s + 32 >= p.n_seg) return r;
+            const int64_t before = __shfl_sync(0xffffffffu, sum, 31);
             s += 32;
+            load(p, before);
         }
-        return r;
     }
 };
 
@@ -346,6 +356,7 @@ __global__ void __launch_bounds__(kThreads, 2) mx_narrow_kernel(const MxProductP
     tc_fence_after();
     const uint32_t tmem = ctrl->tmem;
     if (p.split > 1) cluster_arrive();         // this CTA's barriers are there
+
     // this CTA's tiles, and its share of the channels of each
     const int split = p.split;
     const int rank = split > 1 ? static_cast<int>(blockIdx.x % split) : 0;
@@ -463,7 +474,6 @@ __global__ void __launch_bounds__(kThreads, 2) mx_narrow_kernel(const MxProductP
             const uint32_t acc = tmem + (static_cast<uint32_t>(32 * warp) << 16);
             const int r = 32 * warp + lane;
             bool ok = true;
-
             for (int64_t t = t0; ok; t += step, done++) {
                 const Tile tile = t == first ? head : walk.at(p, t);
                 if (!tile.valid) break;
@@ -599,7 +609,6 @@ struct WideLayout {
     static constexpr int kFactorAt = kTurnAt + 4 * 2 * kTurn, kCtrlAt = kFactorAt + QROWS * 4;
     static constexpr int kBytes = 1024 + kCtrlAt + 256;
     static constexpr int kAccs = QROWS == 256 ? 1 : 2;                       // accumulators
-    static constexpr int kWordCols = Scales<BLOCK>::kWords * 4;              // columns of 128 rows' scales of a stage
     static constexpr int kScaleBase = kAccs * QROWS, kScaleCols = (1 + kQGroups) * 16;
     static constexpr int kColumns = 512;
     static_assert(kScaleBase + kStages * kScaleCols <= kColumns && kBytes <= 227 * 1024, "tensor or shared memory");
