@@ -640,6 +640,8 @@ __device__ __forceinline__ void store_turn(const MxProductParams &p, uint32_t tu
         // Two values a store wherever a row starts: the words between its first and last even places a row at a time, then what
         // that leaves at either end, a lane for each row (ends within the rows' loop: 42 us for 2051 x 2887 x 4096).
         uint16_t *const y = static_cast<uint16_t *>(p.Y);
+        const int odd0 = static_cast<int>(at & 1), turns = static_cast<int>(p.N & 1);             // rows start at even and odd places in turn
+        uint16_t *row = y + at + 2 * lane;
         for (int r0 = 0; r0 < rows; r0 += 8) {
             uint32_t w[8], before[8];                                                                // values 2 lane, 2 lane + 1
 #pragma unroll
@@ -647,11 +649,10 @@ __device__ __forceinline__ void store_turn(const MxProductParams &p, uint32_t tu
 #pragma unroll
             for (int i = 0; i < 8; i++) before[i] = __shfl_up_sync(0xffffffffu, w[i], 1);
 #pragma unroll
-            for (int i = 0; i < 8; i++) {
-                const int64_t to = at + (r0 + i) * p.N;
-                const int odd = static_cast<int>(to & 1), c = 2 * lane - odd;
+            for (int i = 0; i < 8; i++, row += p.N) {
+                const int odd = odd0 ^ (i & turns), c = 2 * lane - odd;
                 const uint32_t two = odd ? __funnelshift_l(before[i], w[i], 16) : w[i];              // values c, c + 1
-                if (r0 + i < rows && c >= 0 && c + 1 < cols) *reinterpret_cast<uint32_t *>(y + to + c) = two;
+                if (r0 + i < rows && c >= 0 && c + 1 < cols) *reinterpret_cast<uint32_t *>(row - odd) = two;
             }
         }
         auto value = [&](int c) {
