@@ -1,0 +1,66 @@
+"""Products of microscaled records where the order of copies, sums and stores matters: call after call, every value
+(needs a B200)."""
+import numpy as np
+import pytest
+import torch
+
+import mx_reference as ref
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def env():
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+    from paper_2608_04991_b200 import binding as rac
+    rac.load()
+    return type("Env", (), dict(rac=rac, dev=torch.device("cuda:0")))
+
+
+def exact_operand(T, d, block, seed, dev):
+    """Records with all scales 1: every partial sum is a multiple of 1/4 below 2^22 (36 d, d up to 32768), which binary32 holds in
+    any order."""
+    rec = ref.random_records(T, d, block, np.random.default_rng(seed))
+    rec[:, d // 2: d // 2 + d // block] = 127 if block == 32 else 0x38
+    if block == 16:
+        rec[:, d // 2 + d // block] = 0
+    return torch.from_numpy(rec).to(dev), torch.from_numpy(ref.decode(rec, d, block)).to(dev)
+
+
+def product_of(a, b, yt):
+    return (a @ b.T).to(torch.float32).to(yt)       # exact in binary32, then the one rounding
+
+
+@pytest.mark.parametrize("block", [16, 32])
+@pytest.mark.parametrize("y", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("M,N,off", [
+    (256 + 149, 10240, None), (256 + 20, 10240, None), (256 + 255, 20480, None),           # a pair's second tile is not full
+    (768 + 149, 4736, None),                                                                 # the same with tiles of 256 x 128
+    (5000, 2048, [0, 300, 700, 1001, 1500, 2300, 2333, 3700, 5000]),                         # tiles that are not full anywhere
+])
+def test_rows_that_end_inside_a_tile_leave_the_tile_before_alone(env, M, N, off, block, y):
+    """A pair of CTAs goes from full tiles, which copies store, to others, which lanes store, through the same buffers; few channels,
+    so that the next sums are there at once."""
+    rac, dev = env.rac, env.dev
+    d = 64
+    n = 1 if off is None else len(off) - 1
+    A, a = exact_operand(M, d, block, 1, dev)
+    B, b = exact_operand(n * N, d, block, 2, dev)
+    cfg = rac.MxCfg(d, block, y_type=y)
+    if off is None:
+        want = product_of(a, b, y)
+    else:
+        want = torch.cat([product_of(a[off[s]:off[s + 1]], b[s * N:(s + 1) * N], y) for s in range(n)])
+        seg_off = torch.tensor(off, dtype=torch.int32, device=dev)
+    status = torch.zeros(1, dtype=torch.int32, device=dev)
+    wrong = torch.zeros(1, dtype=torch.int64, device=dev)
+    Y = torch.empty((M, N), dtype=y, device=dev)
+    for _ in range(100):
+        Y.fill_(-7)
+        if off is None:
+            rac.rac_mx_product(cfg, A, M, B, N, Y, status)
+        else:
+            rac.rac_mx_product_segments(cfg, A, M, seg_off, n, B, N, Y, status)
+        wrong += (Y != want).sum()
+    assert int(wrong) == 0 and int(status) == 0
