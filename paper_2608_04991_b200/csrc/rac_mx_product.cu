@@ -308,6 +308,11 @@ struct NarrowLayout {
     static constexpr int kTx = kP + kQ + kPScale + kQScale;
     static constexpr int kStage = (kTx + 1023) / 1024 * 1024;
     static constexpr int kStages = QROWS == 64 ? 3 : 4;
+    // Two teams of four warps carry scales, a stage each in turn.  In an even ring a team has stages of its own and sees every phase
+    // of them.  In an odd one the stages change hands: both teams see every copy land and say so, or the ring could go on by two
+    // phases before a late warp of the other team has looked, and that warp would wait for a phase that is over.
+    static constexpr bool kOwnStages = kStages % 2 == 0;
+    static constexpr int kReady = kOwnStages ? 4 : 8;                        // warps that a stage waits for
     // split: what the other CTAs of the cluster push, [rank][token][128] (this CTA's own sums lie in the idle stages)
     static constexpr int kPart = (QROWS == 64 ? 60 : 18) * 512;              // the most that (s - 1) * ceil(QROWS / s) is, up to 8
     static constexpr int kPartAt = kStages * kStage, kCtrlAt = kPartAt + kPart;
@@ -339,7 +344,7 @@ __global__ void __launch_bounds__(kThreads, 2) mx_narrow_kernel(const MxProductP
     if (threadIdx.x == 0) {
         for (int i = 0; i < L::kStages; i++) {
             mbar_init(bar(&ctrl->full[i]), 1);
-            mbar_init(bar(&ctrl->ready[i]), 4);
+            mbar_init(bar(&ctrl->ready[i]), L::kReady);
             mbar_init(bar(&ctrl->empty[i]), 1);
         }
         mbar_init(bar(&ctrl->acc_full), 1);
@@ -446,12 +451,16 @@ __global__ void __launch_bounds__(kThreads, 2) mx_narrow_kernel(const MxProductP
                 const Tile tile = t == first ? head : walk.at(p, t);
                 if (!tile.valid) break;
                 for (int ks = ks0; ks < ks1; ks++, it++) {
-                    // both teams wait for every stage: a team that left one out could take its phase for the next but one
                     const int st = it % L::kStages;
+                    const bool mine = (it & 1) == team;
+                    if (L::kOwnStages && !mine) continue;
                     ok = mbar_wait_bounded(bar(&ctrl->full[st]), it / L::kStages & 1);
                     ok = __all_sync(0xffffffffu, ok);
                     if (!ok) break;
-                    if ((it & 1) != team) continue;
+                    if (!mine) {
+                        if (lane == 0) mbar_arrive(bar(&ctrl->ready[st]));
+                        continue;
+                    }
                     tc_fence_after();
                     const uint32_t at = base + st * L::kStage + L::kP + L::kQ + (BLOCK == 32 ? 8 * (ks & 1) : 0);
                     const int left = p.nblk - ks * Scales<BLOCK>::kBytes;

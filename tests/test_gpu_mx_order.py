@@ -64,3 +64,39 @@ def test_rows_that_end_inside_a_tile_leave_the_tile_before_alone(env, M, N, off,
             rac.rac_mx_product_segments(cfg, A, M, seg_off, n, B, N, Y, status)
         wrong += (Y != want).sum()
     assert int(wrong) == 0 and int(status) == 0
+
+
+@pytest.mark.parametrize("block", [16, 32])
+@pytest.mark.parametrize("M,N,d,n", [(64, 6000, 4096, 1), (33, 40000, 1280, 1), (2000, 1000, 1792, 40), (16, 40000, 1280, 1), (200, 1000, 1792, 40)])
+def test_rings_of_three_and_four_stages_keep_in_step(env, M, N, d, n, block):
+    """The narrow form, split over clusters and not, odd numbers of stages a tile, while other calls on another stream take turns on
+    the same SMs."""
+    rac, dev = env.rac, env.dev
+    A, a = exact_operand(M, d, block, 3, dev)
+    B, b = exact_operand(n * N, d, block, 4, dev)
+    cfg = rac.MxCfg(d, block)
+    off = [i * M // n for i in range(n + 1)]
+    seg_off = torch.tensor(off, dtype=torch.int32, device=dev)
+    want = torch.cat([product_of(a[off[s]:off[s + 1]], b[s * N:(s + 1) * N], torch.bfloat16) for s in range(n)])
+    side = torch.cuda.Stream()
+    status = torch.zeros(1, dtype=torch.int32, device=dev)
+    wrong = torch.zeros(1, dtype=torch.int64, device=dev)
+    Y, Z = torch.empty_like(want), torch.empty_like(want)
+    X = torch.ones((4000, d), dtype=torch.bfloat16, device=dev)
+    pay = torch.empty((4000, rac.rac_mx_record_bytes(cfg)), dtype=torch.uint8, device=dev)
+    torch.cuda.synchronize()
+
+    def call(out, **k):
+        if n == 1:
+            rac.rac_mx_product(cfg, A, M, B, N, out, status, **k)
+        else:
+            rac.rac_mx_product_segments(cfg, A, M, seg_off, n, B, N, out, status, **k)
+    for _ in range(60):
+        for _ in range(3):
+            call(Z, stream=side)
+            rac.rac_mx_encode(cfg, X, 4000, pay, pay.numel(), None, None, stream=side)
+        Y.fill_(-7)
+        call(Y)
+        wrong += (Y != want).sum()
+    torch.cuda.synchronize()
+    assert int(wrong) == 0 and int(status) == 0 and torch.equal(Z, want)

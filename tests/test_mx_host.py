@@ -116,3 +116,47 @@ def test_reference_rounds_to_the_nearest_code_and_clips_nothing(block):
     assert np.array_equal(np.abs(v - x), best)
     assert (np.abs(x) <= 6 * s).all()
     assert np.array_equal(np.signbit(v), np.signbit(x) & (v != 0))
+
+
+def narrow_ring(stages, own_only, both_arrive, steps=9):
+    """Every order of events in the narrow product's ring: copies (issued when a stage is free, landing in any order), one warp of
+    either scale team, the matrix thread.  A wait for copy i's phase of its stage ends as soon as the parity of the stage's
+    finished phases says so.  Returns what goes wrong, or None."""
+    start = (frozenset(), 0, 0, 0, 0)             # landed, issued, multiplied, the teams' places
+    seen, todo = {start}, [start]
+    while todo:
+        landed, issued, done, *at = state = todo.pop()
+        after = []
+        if issued < steps and (issued < stages or done > issued - stages):
+            after.append((landed, issued + 1, done, *at))
+        after += [(landed | {i}, issued, done, *at) for i in range(issued) if i not in landed]
+        for team in (0, 1):
+            i = at[team]
+            if i == steps:
+                continue
+            on = (landed, issued, done, *(at[k] + (k == team) for k in (0, 1)))
+            phases = sum(1 for j in landed if j % stages == i % stages)
+            if own_only and i % 2 != team:
+                after.append(on)
+            elif phases % 2 != i // stages % 2:
+                if i not in landed:
+                    return "a phase was taken for another"
+                after.append(on)
+        if done in landed and at[done % 2] > done and (not both_arrive or min(at) > done):
+            after.append((landed, issued, done + 1, *at))
+        if not after and (done, *at) != (steps, steps, steps):
+            return "a wait can only run out"
+        for s in after:
+            if s not in seen:
+                seen.add(s)
+                todo.append(s)
+    return None
+
+
+def test_the_rings_of_the_narrow_product_cannot_miss_a_phase():
+    """As the kernel has them (3 stages: both teams arrive; 4: a team looks at its own stages only), and why not otherwise."""
+    assert narrow_ring(3, own_only=False, both_arrive=True) is None
+    assert narrow_ring(4, own_only=True, both_arrive=False) is None
+    assert narrow_ring(3, own_only=False, both_arrive=False) == "a wait can only run out"
+    assert narrow_ring(4, own_only=False, both_arrive=False) == "a wait can only run out"
+    assert narrow_ring(3, own_only=True, both_arrive=False) == "a phase was taken for another"
