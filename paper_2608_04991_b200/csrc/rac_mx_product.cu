@@ -939,14 +939,17 @@ __global__ void __launch_bounds__(kThreads, 1) mx_wide_kernel(const MxProductPar
                 if (p.y_maps && mine == 32) {
                     fence_async_smem();
                     __syncwarp();
-                    if (lane == 0) tma_store_2d(&maps.y, static_cast<int>(tile.n0) + c0, static_cast<int>(row0) + 32 * warp, turn);
+                    if (lane == 0) {
+                        tma_store_2d(&maps.y, static_cast<int>(tile.n0) + c0, static_cast<int>(row0) + 32 * warp, turn);
+                        bulk_commit();
+                    }
                 } else {
                     // rows that are not all this segment's, or that start where TMA cannot
                     __syncwarp();
                     store_turn(p, turn, mine, (row0 + 32 * warp) * p.N + tile.n0 + c0, min(per, cols - c0));
                     __syncwarp();
+                    if (lane == 0) bulk_commit();      // a group a turn, here without a copy: the wait above counts turns
                 }
-                if (lane == 0) bulk_commit();          // a group a turn, one without a copy too: the wait above counts turns
             }
             tc_fence_before();
             __syncwarp();
