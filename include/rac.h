@@ -498,7 +498,7 @@ int rac_mx_product(const rac_mx_cfg *cfg, const void *A, int64_t M, const void *
 int rac_mx_product_segments(const rac_mx_cfg *cfg, const void *A, int64_t M, const int32_t *seg_off, int64_t n_seg,
                             const void *B, int64_t N, void *Y, uint32_t *dev_status, void *stream);
 
-/* Self-test of the products' bounded waits, like rac_selftest_bounded_wait: rac_mx_product (M and N at most 1024) with every
+/* Self-test of the products' bounded waits, like rac_selftest_bounded_wait: rac_mx_product (M and N at most 4096) with every
  * stage announcing 16 bytes more than its copies deliver.  Expected: RAC_OK from the call, RAC_STATUS_TIMEOUT in *dev_status, Y
  * unspecified, and the stream usable afterwards. */
 int rac_mx_selftest_bounded_wait(const rac_mx_cfg *cfg, const void *A, int64_t M, const void *B, int64_t N, void *Y,

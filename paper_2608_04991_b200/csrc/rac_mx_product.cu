@@ -628,6 +628,13 @@ struct WideCtrl {
     int abort;
 };
 
+// whether all 128 threads of the epilogue say so; a barrier for them
+__device__ __forceinline__ bool epilogue_all(bool mine) {
+    uint32_t all;
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbar.red.and.pred q, 1, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                 : "=r"(all) : "r"(static_cast<uint32_t>(mine)) : "memory");
+    return all != 0;
+}
 // `rows` rows of 128 bytes of Y from shared memory (16-byte piece q of row r at q ^ (r mod 8)) to rows of `cols` values that start
 // at `at` and are p.N values apart.
 __device__ __forceinline__ void store_turn(const MxProductParams &p, uint32_t turn, int rows, int64_t at, int cols) {
@@ -854,7 +861,7 @@ __global__ void __launch_bounds__(kThreads, 1) mx_wide_kernel(const MxProductPar
         const bool wide_y = p.y_type == RAC_MX_FP32;
         const int per = wide_y ? 32 : 64;          // values of a row of Y per turn
         int turns = 0;
-        for (int64_t t = first; ok; t += step, done++) {
+        for (int64_t t = first;; t += step, done++) {
             const Tile tile = t == first ? head : walk.at(p, t);
             if (!tile.valid) break;
             const int64_t row0 = tile.lo + rank * kRows;
@@ -862,11 +869,14 @@ __global__ void __launch_bounds__(kThreads, 1) mx_wide_kernel(const MxProductPar
             const int cols = static_cast<int>(min(p.N - tile.n0, static_cast<int64_t>(QROWS)));
             const int ab = done % L::kAccs;
             const uint32_t acc = tmem + ab * QROWS + (static_cast<uint32_t>(32 * warp) << 16);
+            // a warp whose wait ran out takes the others with it: nobody is left behind at a barrier of four (block 16: the tile
+            // before has read its factors, too)
+            if (BLOCK == 16) ok = epilogue_all(ok);
+            if (!ok) break;
             int e = 0;
             bool plain = true;                     // exponents so small that their factors multiply without loss
             if (BLOCK == 16) {
                 const uint8_t *a = p.A + row0 * p.rec, *b = p.B + (tile.matrix + tile.n0) * p.rec;
-                asm volatile("bar.sync 1, 128;" ::: "memory");           // the tile before has read its factors
                 e = r < rows ? mx_row_exp(a + r * static_cast<int64_t>(p.rec), exp_off) : 0;
                 plain = e >= -50 && e <= 50;
                 for (int c = r; c < QROWS; c += 128) {
@@ -874,10 +884,7 @@ __global__ void __launch_bounds__(kThreads, 1) mx_wide_kernel(const MxProductPar
                     factor[c] = __int_as_float(eb);
                     plain = plain && eb >= -50 && eb <= 50;
                 }
-                uint32_t all;
-                asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbar.red.and.pred q, 1, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
-                             : "=r"(all) : "r"(static_cast<uint32_t>(plain)) : "memory");
-                plain = all != 0;
+                plain = epilogue_all(plain);
                 if (plain) {
                     for (int c = r; c < QROWS; c += 128) factor[c] = mx_pow2(__float_as_int(factor[c]));
                     asm volatile("bar.sync 1, 128;" ::: "memory");
@@ -885,7 +892,7 @@ __global__ void __launch_bounds__(kThreads, 1) mx_wide_kernel(const MxProductPar
             }
             ok = mbar_wait_bounded(bar(&ctrl->acc_full[ab]), done / L::kAccs & 1) && !aborted();
             ok = __all_sync(0xffffffffu, ok);
-            if (!ok) break;
+            if (!ok) continue;
             tc_fence_after();
             const float fa = plain ? mx_pow2(e) : 0.0f;
             const int mine = min(32, rows - 32 * warp);                  // rows of this warp
@@ -1127,7 +1134,7 @@ int rac_mx_product_segments(const rac_mx_cfg *cfg, const void *A, int64_t M, con
 
 int rac_mx_selftest_bounded_wait(const rac_mx_cfg *cfg, const void *A, int64_t M, const void *B, int64_t N, void *Y,
                                  uint32_t *dev_status, void *stream) {
-    if (M > 1024 || N > 1024) return RAC_EUNSUPPORTED;
+    if (M > 4096 || N > 4096) return RAC_EUNSUPPORTED;
     return mx_product_impl(cfg, A, M, nullptr, 1, B, N, Y, dev_status, stream, 16);
 }
 

@@ -100,3 +100,21 @@ def test_rings_of_three_and_four_stages_keep_in_step(env, M, N, d, n, block):
         wrong += (Y != want).sum()
     torch.cuda.synchronize()
     assert int(wrong) == 0 and int(status) == 0 and torch.equal(Z, want)
+
+
+@pytest.mark.parametrize("block", [16, 32])
+@pytest.mark.parametrize("M,N,d", [(4096, 4096, 256), (4096, 4096, 4096), (3328, 1408, 512)])
+def test_waits_that_cannot_complete_end_with_a_status_before_the_last_tile(env, M, N, d, block):
+    """Pairs of CTAs with more tiles to go (256 x 256 and 256 x 128): their warps give up at different times."""
+    rac, dev = env.rac, env.dev
+    A, a = exact_operand(M, d, block, 1, dev)
+    B, b = exact_operand(N, d, block, 2, dev)
+    cfg = rac.MxCfg(d, block)
+    Y = torch.empty((M, N), dtype=torch.bfloat16, device=dev)
+    status = torch.zeros(1, dtype=torch.int32, device=dev)
+    rac.rac_mx_selftest_bounded_wait(cfg, A, M, B, N, Y, status)
+    torch.cuda.synchronize()
+    assert int(status) == rac.STATUS_TIMEOUT
+    status.zero_()
+    rac.rac_mx_product(cfg, A, M, B, N, Y, status)          # the device is as it was
+    assert int(status) == 0 and torch.equal(Y, product_of(a, b, torch.bfloat16))
