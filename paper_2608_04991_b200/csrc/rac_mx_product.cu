@@ -530,8 +530,8 @@ __global__ void __launch_bounds__(kThreads, 2) mx_narrow_kernel(const MxProductP
             if (threadIdx.x == 0) mbar_arrive_expect_tx(bar(&ctrl->parts), static_cast<uint32_t>((split - 1) * mine * 512));
             const int eb = BLOCK == 16 && n < cols ? mx_row_exp(b + n * static_cast<int64_t>(p.rec), exp_off) : 0;
             int ea = BLOCK == 16 && lane < mine ? mx_row_exp(a + lane * static_cast<int64_t>(p.rec), exp_off) : 0;
-            bool ok = mbar_wait_bounded(bar(&ctrl->acc_full), done & 1);
-            ok = __all_sync(0xffffffffu, ok) && !aborted();
+            bool ok = mbar_wait_bounded(bar(&ctrl->acc_full), done & 1) && !aborted();
+            ok = __all_sync(0xffffffffu, ok);          // one answer a warp, what it read of the flag included
             tc_fence_after();
             if (ok) {
                 for (int c = 0; c < rows; c += 16) {
