@@ -767,9 +767,12 @@ __global__ void __launch_bounds__(kThreads, 1) mx_wide_kernel(const MxProductPar
             }
             ok = __shfl_sync(0xffffffffu, ok, 0);
         }
-        if (!ok && lane == 0) {      // copies in flight must land before the CTA's memory is given back
-            for (int i = max(0, it - L::kStages); i < it; i++) mbar_wait_bounded(bar(&ctrl->full[i % L::kStages]), i / L::kStages & 1);
-            for (int i = max(0, group - 2); i < group; i++) mbar_wait_bounded(bar(&ctrl->scale_full[i & 1]), i >> 1 & 1);
+        // Before the CTA's memory is given back the last stages' arrivals have come (the first CTA's matrix instructions make them,
+        // with no regard to the barriers at the end), or, where a wait ran out, the copies in flight have landed.
+        if (lane == 0) {
+            for (int i = max(0, it - L::kStages); i < it; i++)
+                mbar_wait_bounded(bar(ok ? &ctrl->empty[i % L::kStages] : &ctrl->full[i % L::kStages]), i / L::kStages & 1);
+            for (int i = max(0, group - 2); !ok && i < group; i++) mbar_wait_bounded(bar(&ctrl->scale_full[i & 1]), i >> 1 & 1);
         }
     } else if (warp == 13) {
         // ---- matrix instructions, for both CTAs
@@ -797,6 +800,10 @@ __global__ void __launch_bounds__(kThreads, 1) mx_wide_kernel(const MxProductPar
                 if (!ok) mbar_wait_bounded(bar(&ctrl->acc_full[ab]), done / L::kAccs & 1);
             }
             ok = __shfl_sync(0xffffffffu, ok, 0);
+        }
+        // the other CTA's last arrivals have come: the barrier at the end orders none of them
+        if (lane == 0 && ok) {
+            for (int i = max(0, done - L::kAccs); i < done; i++) mbar_wait_bounded(bar(&ctrl->acc_empty[i % L::kAccs]), i / L::kAccs & 1);
         }
     } else if (warp >= 4) {
         // ---- scales, a quarter of the lanes each; two teams of four warps take turns, a stage each

@@ -118,3 +118,29 @@ def test_waits_that_cannot_complete_end_with_a_status_before_the_last_tile(env, 
     status.zero_()
     rac.rac_mx_product(cfg, A, M, B, N, Y, status)          # the device is as it was
     assert int(status) == 0 and torch.equal(Y, product_of(a, b, torch.bfloat16))
+
+
+@pytest.mark.parametrize("block", [16, 32])
+def test_short_products_back_to_back(env, block):
+    """One tile a pair or cluster and the next call's CTAs behind it on the same SMs: what one still sends to its neighbour must not
+    reach those.  Every result of a row of calls of all forms."""
+    rac, dev = env.rac, env.dev
+    d = 256
+    cfg = rac.MxCfg(d, block)
+    B, b = exact_operand(2304, d, block, 2, dev)
+    ops = [exact_operand(m, d, block, m, dev) for m in (300, 5, 2048, 40, 512, 700)]
+    want = [product_of(a, b, torch.bfloat16) for _, a in ops]
+    status = torch.zeros(1, dtype=torch.int32, device=dev)
+    wrong = torch.zeros(1, dtype=torch.int64, device=dev)
+    outs = [[torch.empty_like(w) for w in want] for _ in range(8)]
+    for _ in range(20):
+        for row in outs:
+            for y in row:
+                y.fill_(-7)
+        for row in outs:
+            for (A, _), y in zip(ops, row):
+                rac.rac_mx_product(cfg, A, A.shape[0], B, 2304, y, status)
+        for row in outs:
+            for w, y in zip(want, row):
+                wrong += (y != w).sum()
+    assert int(wrong) == 0 and int(status) == 0
