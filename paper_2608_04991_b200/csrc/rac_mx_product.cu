@@ -353,12 +353,13 @@ __global__ void __launch_bounds__(kThreads, 2) mx_narrow_kernel(const MxProductP
         ctrl->abort = 0;
         mbar_init_fence();
     }
-    if (p.early) grid_launch_dependents();
     if (warp == 12 && lane < 4) tma_prefetch(&maps.a + lane);
     if (warp == 13) tc_alloc<false, L::kColumns>(smem_u32(&ctrl->tmem));
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
+    // not before this CTA has its columns: one of the next kernel's might take them and wait for this grid's end
+    if (p.early) grid_launch_dependents();
     const uint32_t tmem = ctrl->tmem;
     if (p.split > 1) cluster_arrive();         // this CTA's barriers are there
 
@@ -711,7 +712,6 @@ __global__ void __launch_bounds__(kThreads, 1) mx_wide_kernel(const MxProductPar
         ctrl->abort = 0;
         mbar_init_fence();
     }
-    if (p.early) grid_launch_dependents();
     if (warp == 12 && lane < 4 + p.y_maps) tma_prefetch(&maps.a + lane);
     if (warp == 13) tc_alloc<true, L::kColumns>(smem_u32(&ctrl->tmem));
     tc_fence_before();
@@ -719,6 +719,8 @@ __global__ void __launch_bounds__(kThreads, 1) mx_wide_kernel(const MxProductPar
     cluster_arrive();                                    // this CTA's barriers are there, and the other's
     cluster_wait();
     tc_fence_after();
+    // not before this CTA has its columns: one of the next kernel's might take them and wait for this grid's end
+    if (p.early) grid_launch_dependents();
     const uint32_t tmem = ctrl->tmem;
 
     const int64_t first = blockIdx.x / 2, step = gridDim.x / 2;

@@ -144,3 +144,37 @@ def test_short_products_back_to_back(env, block):
             for w, y in zip(want, row):
                 wrong += (y != w).sum()
     assert int(wrong) == 0 and int(status) == 0
+
+
+@pytest.mark.parametrize("M", [3, 64, 300])
+def test_products_beside_other_kernels_that_use_tensor_memory(env, M):
+    """A library's matrix products before, behind and beside these, captured and replayed: both want the SMs' tensor memory."""
+    rac, dev = env.rac, env.dev
+    cfg = rac.MxCfg(1280, 16)
+    (A, a), (B, b) = exact_operand(M, 1280, 16, 1, dev), exact_operand(2000, 1280, 16, 2, dev)
+    want = product_of(a, b, torch.bfloat16)
+    U = torch.eye(2048, dtype=torch.bfloat16, device=dev)
+    status = torch.zeros(1, dtype=torch.int32, device=dev)
+    outs = [torch.empty_like(want) for _ in range(6)]
+
+    def run():
+        V = U
+        for y in outs:
+            rac.rac_mx_product(cfg, A, M, B, 2000, y, status)
+            V = V @ U
+        return V
+    run()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        V = run()
+    side = torch.cuda.Stream()
+    for _ in range(30):
+        for y in outs:
+            y.fill_(-7)
+        graph.replay()
+        with torch.cuda.stream(side):
+            U @ U
+        torch.cuda.synchronize()
+        assert all(torch.equal(y, want) for y in outs)
+    assert int(status) == 0 and torch.equal(V, U)
