@@ -199,11 +199,11 @@ __global__ void __launch_bounds__(512, CHUNKS > 1 ? 1 : STAY ? 3 : 4) mx_encode_
                 s = f ? mx_e8m0(byte) : 0.0f;
                 inv = __uint_as_float((254u - byte) << 23);
             } else {
-                const float b = a * mx_pow2(-rexp);                  // exact
+                const float b = a * mx_pow2(-rexp);                  // exact, or so small that the first scale serves
                 uint16_t q;                                          // nearest e4m3, then the next one where that is too small
                 asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(q) : "f"(0.0f), "f"(b * (1.0f / 6.0f)));
                 byte = q & 127u;
-                byte += 6.0f * mx_e4m3(byte) < b;
+                byte += mx_e4m3(byte) * (6.0f * mx_pow2(rexp)) < a;  // both exact; a itself, which is not 0 where b may be
                 const float v = mx_e4m3(byte);
                 s = v * mx_pow2(rexp);
                 asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(v > 0.0f ? v : 1.0f));        // off by an ulp at most; v is no less than 2^-9
