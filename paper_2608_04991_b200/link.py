@@ -166,10 +166,14 @@ class EntryProduct:
 
     def __init__(self, W: torch.Tensor, block: int = 16):
         from . import binding as rac
+        if W.dim() != 2:
+            raise ValueError(f"weights: expected [N, d], got {tuple(W.shape)}")
         self.rac = rac
-        self.N, d = W.shape
-        self.cfg = rac.MxCfg(d, block)
+        self.N, self.d = W.shape
+        self.cfg = rac.MxCfg(self.d, block)
         self.rec = rac.rac_mx_record_bytes(self.cfg)
+        if self.rec == 0:
+            raise ValueError(f"unsupported configuration {self.cfg!r}")
         self.status = torch.zeros(1, dtype=torch.int32, device=W.device)
         self.records = self._encode(W)
         self.check()
@@ -180,6 +184,8 @@ class EntryProduct:
         return records
 
     def __call__(self, x_hat: torch.Tensor) -> torch.Tensor:
+        if x_hat.dim() != 2 or x_hat.shape[1] != self.d:
+            raise ValueError(f"states: expected [T, {self.d}], got {tuple(x_hat.shape)}")
         T = x_hat.shape[0]
         Y = torch.empty((T, self.N), dtype=torch.bfloat16, device=x_hat.device)
         self.rac.rac_mx_product(self.cfg, self._encode(x_hat), T, self.records, self.N, Y, self.status)

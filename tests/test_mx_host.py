@@ -160,3 +160,23 @@ def test_the_rings_of_the_narrow_product_cannot_miss_a_phase():
     assert narrow_ring(3, own_only=False, both_arrive=False) == "a wait can only run out"
     assert narrow_ring(4, own_only=False, both_arrive=False) == "a wait can only run out"
     assert narrow_ring(3, own_only=True, both_arrive=False) == "a phase was taken for another"
+
+
+def test_entry_product_takes_rows_of_its_weights_width_only(rac, monkeypatch):
+    """States of another width would be read with the weights' record length, out of range where they are narrower."""
+    from paper_2608_04991_b200 import link
+    calls = []
+    for name in ("rac_mx_encode", "rac_mx_product"):
+        monkeypatch.setattr(rac, name, lambda *a, name=name, **k: calls.append(name))
+    entry = link.EntryProduct(torch.zeros((40, 128), dtype=torch.bfloat16))
+    calls.clear()
+    for shape in ((7, 96), (7, 160), (128,), (2, 7, 128), (7, 0)):
+        with pytest.raises(ValueError, match="128"):
+            entry(torch.zeros(shape, dtype=torch.bfloat16))
+    assert calls == []
+    for T in (0, 1, 7):
+        assert entry(torch.zeros((T, 128), dtype=torch.bfloat16)).shape == (T, 40)
+    assert calls == ["rac_mx_encode", "rac_mx_product"] * 3
+    for bad in (torch.zeros(128, dtype=torch.bfloat16), torch.zeros((4, 40), dtype=torch.bfloat16), torch.zeros((4, 32800), dtype=torch.bfloat16)):
+        with pytest.raises(ValueError):
+            link.EntryProduct(bad)
