@@ -430,9 +430,10 @@ int rac_recon_error(const void *X, const void *X_hat, int64_t T, int32_t d, doub
  *
  * The paper sends a state that has no reference yet (the first decode step, Sec. IV-B before Eq. 5) as it stands, and its own
  * quantiser is an integer one against a reference.  These calls are this library's direct form beside it: a record
- * holds a row in a form that the tensor cores multiply as it stands, so the partition behind the boundary can take its
- * first product from what came over the link.  Rows are states or rows of a weight matrix: both operands of a product
- * have the same records.
+ * holds a row in a form that the tensor cores multiply as it stands.  The partition behind the boundary can take its first
+ * product from such records, whether they came over a link or were coded from what an end reconstructed (link.EntryProduct
+ * does the latter: what link.py sends are the integer codec's records).  Rows are states or rows of a weight matrix:
+ * both operands of a product have the same records.
  *
  * Record of one row of d values (little endian), records back to back:
  *     codes   d/2 B        e2m1 code of channel c in bits 4*(c%2) .. +3 of byte c/2: sign, two bits of exponent, one of

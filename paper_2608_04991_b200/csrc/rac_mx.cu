@@ -3,8 +3,8 @@
 //
 // Both kernels stream: a thread has 16 consecutive channels (one block of 16, half a block of 32), a CTA has as many whole
 // rows as fit its threads.  What bounds them is memory: 2 bytes in and 0.57 (+ 2 with x_hat) out per value.  131072 x 5120, blocks
-// of 16: encode with x_hat 476 us in short bursts (6.4 TB/s; 536 us in a sustained run, where power counts), without 340 us (there
-// instruction issue bounds it), decode 291 us (5.9 TB/s).
+// of 16: encode with x_hat 477 us in short bursts (6.4 TB/s; 506 to 536 us in sustained runs, where power counts), without 333 us
+// (there instruction issue bounds it), decode 293 us (5.9 TB/s).
 #include "rac_mx.cuh"
 
 namespace rac {

@@ -12,12 +12,16 @@
 //   wide    many rows: a pair of CTAs makes a tile of 256 rows of A by 256 (128) of B with cta_group::2, so that each CTA loads
 //           half of either operand (38 KB a stage, 54 KB for a tile of 128 x 256 by one CTA, whose loads alone took 214 us of the
 //           size above).  Rows of A are the lanes of the accumulator: a thread holds consecutive values of a row of Y.
-//           Persistent pairs.  210 us (4.1 PFLOP/s) in short bursts; in a sustained run the power limit holds it at 256 us.
+//           Persistent pairs.  213 us (4.0 PFLOP/s; blocks of 32: 187) in short bursts; in a sustained run the power limit holds it
+//           at 250 us.
 //   narrow  few rows (a decode step, a segment of a few tokens): a tile is 128 rows of B by up to 64 of A, so the weights
 //           fill the 128 lanes and a handful of tokens costs a handful of columns.  What bounds it is the weights' way in, a
 //           ring of copies whose round trips are 1.5 to 2.5 us, and for a single token the set-up and the sums' exchange;
 //           where the tiles alone do not fill the SMs, clusters split the channels and add their partial sums through
-//           distributed shared memory in a fixed order.  1 x 4096 x 4096: 6.6 us; 64 x 5120 x 5120: 10.6 us.
+//           distributed shared memory in a fixed order.  1 x 4096 x 4096: 6.6 us; 64 x 5120 x 5120: 10.7 us.  Two CTAs an SM leave 72
+//           registers a thread; 92 to 112 bytes a thread go through local memory.
+// Times in this file are of blocks of 16 unless stated otherwise, on the device: a call out of 20 in a captured graph that is replayed
+// alone, operands in L2 where they fit.  Passes one behind the other through the binding: 6.9 us for one token of 4096 x 4096.
 // Warps 0-3 of a CTA are the epilogue, 4-11 carry scales, the next issues TMA loads and the last the matrix
 // instructions.  Every wait on an mbarrier is bounded: a copy that never lands ends the kernel with RAC_STATUS_TIMEOUT.
 #include <cuda.h>
@@ -655,8 +659,8 @@ __device__ __forceinline__ void store_turn(const MxProductParams &p, uint32_t tu
             if (lane < cols) y[r * p.N] = __uint_as_float(lds32(turn + r * 128 + ((lane >> 2) ^ (r & 7)) * 16 + (lane & 3) * 4));
     } else {
         // Two values a store wherever a row starts: the words between its first and last even places a row at a time, then what
-        // that leaves at either end, a lane for each row (2051 x 2887 x 4096: 27.3 us; with the ends within the
-        // rows' loop 42; 2888 features, which TMA stores, 20.5).
+        // that leaves at either end, a lane for each row (2051 x 2887 x 4096, blocks of 32: 27.4 us; with the ends
+        // within the rows' loop 42; 2888 features, which TMA stores, 20.5).
         uint16_t *const y = static_cast<uint16_t *>(p.Y);
         const int odd0 = static_cast<int>(at & 1), turns = static_cast<int>(p.N & 1);             // rows start at even and odd places in turn
         uint16_t *row = y + at + 2 * lane;
@@ -1035,9 +1039,9 @@ static int launch_narrow(MxProductParams p, int sms, cudaStream_t s) {
         return RAC_ECUDA;
     p.n_tiles = static_cast<int>((p.N + kRows - 1) / kRows);
     const int64_t tiles = row_tiles(p, QROWS) * p.n_tiles;
-    // CTAs of clusters: one per SM where a tile is a few tokens (1 x 4096 x 4096: 128 CTAs 5.8 us, 256 6.1; 1 x 5120 x 5120: 120 CTAs
-    // 7.1, 240 7.4, 280, which do not all fit beside one another in clusters, 11.5), more where the tokens are work, too
-    // (64 x 5120 x 5120: 120 CTAs 12.2, 240 10.1).
+    // CTAs of clusters: one per SM where a tile is a few tokens (1 x 4096 x 4096: 128 CTAs 6.6 us, 256 6.8; 1 x 5120 x 5120: 120 and
+    // 240 CTAs 7.8, 280, which do not all fit beside one another in clusters, 12.2), more where the tokens are work, too
+    // (64 x 5120 x 5120: 120 CTAs 12.8, 240 10.7, 280 18.3).
     const int64_t together = QROWS == 16 ? sms : sms * 5 / 3, slots = 2 * sms;
     p.split = 1;
     while (p.split < L::kMaxSplit && tiles * (p.split + 1) <= together && p.split < p.k_stages) p.split++;
@@ -1076,9 +1080,13 @@ static int dispatch_mx_product(const MxProductParams &p, cudaStream_t s) {
     const int sms = mx_sm_count();
     if (sms <= 0) return RAC_ECUDA;
     // By the rows that a weight matrix has, on average.  Few: their own width.  More: the narrow form where its tiles are few
-    // enough to be split among five CTAs or more (128 x 1024 x 4096: 8.0 us, wide 10.9), else tiles of 256 x 128 or 256 x 256,
+    // enough to be split among five CTAs or more (128 x 1024 x 4096: 8.8 us, wide 10.4), else tiles of 256 x 128 or 256 x 256,
     // whichever takes less time in rounds of all pairs, a stage of the former taking 0.8 times as long as the latter's
-    // (256 x 5120 x 5120, one round of either: 12.9 and 14.8 us; 512 rows, two rounds and one: 20.5 and 15.0 us).
+    // (256 x 5120 x 5120, one round of either: 12.4 and 14.2 us; 512 rows, two rounds and one: 21.3 and 14.9 us).
+    // The lengths of segments are on the device, so uneven ones go by their mean.  32 matrices of 2880 x 2880 (blocks of 32), tiles of 16 /
+    // 64 rows of A / 256 x 256: 16 rows each 30 / 32 / 58 us, 64 each 71 / 39 / 53, 65 each 85 / 50 / 57, 128 each 133 / 56 / 54; one segment
+    // of 1550 and 31 of 16 (mean 64) 78 / 52 / 65, one of 300 and 31 of 4 (mean 14) 38 / 35 / 56; 16 matrices, one of 2000 rows and 15
+    // of 8 (mean 133) 76 / 40 / 36.  2048 x 4096 in blocks of 16, 65 each: 94 / 66 / 57.  At its worst the choice costs an eighth.
     const int64_t rows = (p.M + p.n_seg - 1) / p.n_seg, pairs = sms / 2 > 0 ? sms / 2 : 1;
     if (rows <= 16) return launch_narrow<BLOCK, 16>(p, sms, s);
     if (rows <= 64 || row_tiles(p, 64) * ((p.N + kRows - 1) / kRows) <= sms / 3) return launch_narrow<BLOCK, 64>(p, sms, s);
