@@ -807,8 +807,8 @@ __global__ void __launch_bounds__(kThreads, 1) mx_wide_kernel(const MxProductPar
             }
             ok = __shfl_sync(0xffffffffu, ok, 0);
         }
-        // the other CTA's last arrivals have come: the barrier at the end orders none of them
-        if (lane == 0 && ok) {
+        // the other CTA's last arrivals have come, or will not any more: the barrier at the end orders none of them
+        if (lane == 0) {
             for (int i = max(0, done - L::kAccs); i < done; i++) mbar_wait_bounded(bar(&ctrl->acc_empty[i % L::kAccs]), i / L::kAccs & 1);
         }
     } else if (warp >= 4) {
